@@ -17,7 +17,8 @@
  *     that uses them has finished on the stream.
  *   - Arrays are dense, row-major, 4-byte elements (fp32, int32, uint32),
  *     rank 0..2, at most ACC_MAX_ELEMENTS (2^31 - 2^16) elements, base pointers
- *     16-byte aligned.
+ *     16-byte aligned.  Arrays that only operators (below) read and write may
+ *     also have 2-byte elements (fp16, bf16).
  *   - A graph handle is not thread-safe.
  */
 #ifndef ACC_H
@@ -50,10 +51,22 @@ enum acc_kind {
                       off is S+1 increasing int offsets read by index (the paper names foldSeg in a keyword
                       list only; segments must be non-empty since a fold has no seed)          */
   ACC_SCANL,       /* inclusive left-to-right scan per innermost row  slots {xs}  */
-  ACC_SCANR        /* inclusive right-to-left scan per innermost row  slots {xs}  */
+  ACC_SCANR,       /* inclusive right-to-left scan per innermost row  slots {xs}  */
+  /* Operators: foreign functions in the sense of Section 3.4, arrays that one
+   * kernel of their own computes from whole arrays.  Every edge into and out of
+   * an operator is infusible, so it is always a cluster of its own; it needs no
+   * instantiation.  See "operators" below for what each one computes.           */
+  ACC_BLOCK_TABLE,     /* slots {lens, free} or {lens, free, old_lens, old}       */
+  ACC_SLOT_MAP,        /* slots {table, lens, off}                                */
+  ACC_PUT_ROWS,        /* slots {dest, slots, rows}                               */
+  ACC_PAGED_ATTENTION, /* slots {q, keys, values, table, lens}                    */
+  ACC_PENALIZE         /* slots {logits, tokens, params, bias_ids, bias, mask}    */
 };
 
-enum acc_dtype { ACC_F32 = 0, ACC_I32 = 1, ACC_U32 = 2 };
+enum acc_dtype {
+  ACC_F32 = 0, ACC_I32 = 1, ACC_U32 = 2,
+  ACC_F16 = 3, ACC_BF16 = 4 /* inputs and results of operators only: combinators are built for 4-byte elements */
+};
 
 /* Element functions (the paper leaves them abstract; these are the ones the
  * build instantiates).  fp32 functions round after every operation (no FMA
@@ -135,7 +148,7 @@ enum acc_status {
   ACC_ERR_WORKSPACE = -12,         /* workspace null, misaligned or too small               */
   ACC_ERR_CUDA = -13,              /* a CUDA runtime call failed                            */
   ACC_ERR_DEVICE_TIMEOUT = -14,    /* a bounded device-side wait ran out                    */
-  ACC_ERR_INDEX_RANGE = -15,       /* scatter index outside its destination                 */
+  ACC_ERR_INDEX_RANGE = -15,       /* scatter index outside its destination, or another number that an operator reports */
   ACC_ERR_TOO_LARGE = -16,         /* graph too large for the requested planner mode        */
   ACC_ERR_NO_PARTITION = -17       /* acc_run(FUSED) before a clustering was set            */
 };
@@ -174,8 +187,9 @@ int acc_graph_create(acc_graph** out);
 int acc_graph_destroy(acc_graph* g);
 /* Appends a node.  Every input must be an existing node, so the graph is a DAG
  * in node-id order.  Edges are classified here: infusible out of an INPUT,
- * into a free-variable slot, into PERMUTE's defaults slot, out of a PERMUTE
- * and through a forced slot (Sections 3.4 and 4.1); fusible otherwise.
+ * into a free-variable slot, into PERMUTE's defaults slot, out of a PERMUTE,
+ * through a forced slot (Sections 3.4 and 4.1), into and out of an operator;
+ * fusible otherwise.
  * The descriptor is copied. */
 acc_node acc_add_node(acc_graph* g, const acc_node_desc* d);
 /* Marks a node as a program output: its array is manifest under every clustering. */
@@ -185,6 +199,65 @@ int32_t acc_node_count(const acc_graph* g);
 /* Writes the fusible edges as pairs (a,b) into F and the infusible ones into I
  * (each up to `cap` pairs, 2*cap int32); *nF and *nI receive the true counts. */
 int acc_edges(const acc_graph* g, int32_t* F, int32_t* nF, int32_t* I, int32_t* nI, int32_t cap);
+
+/* ---- operators ------------------------------------------------------------------
+ *
+ * What a step of a language model that answers needs next to its dense products,
+ * as nodes of a program.  All slots are array slots (n_array_inputs = n_inputs),
+ * fn_id and idx_fn_id are 0, integer arrays are I32 or U32 (read as signed).
+ * An extent of zero is allowed wherever a shape is given.  What a run finds wrong
+ * in the data (a number outside its range) it reports as ACC_ERR_INDEX_RANGE from
+ * acc_finish; nothing outside the arrays is read or written then.
+ *
+ * The cache of keys or values is a rank-2 array of S rows, one per token (a
+ * slot), of all heads side by side; blocks of `block` consecutive slots are handed
+ * out to requests.  block = iparam[0] >= 1 for the three operators that use it.
+ *
+ * BLOCK_TABLE {lens[R], free[N]} -> table[R, W]
+ *     Row r names the ceil(lens[r] / block) blocks of request r, taken in order of
+ *     the requests from the front of `free`; the rest of the row is -1.
+ *   {lens[R], free[N], old_lens[R], old[R, W]}: request r keeps the blocks that its
+ *     old length needed (as far as the new one needs them) and only further ones
+ *     come from `free`.  May be bound in place of `old`.
+ *     Reported: a negative length, a row of more than W blocks, more blocks than N
+ *     (the entries that there is no block for are -1).
+ * SLOT_MAP {table[R, W], lens[R], off[R + 1]} -> slots[T]
+ *     New token t of the packed batch, off[r] <= t < off[r + 1], is the token at
+ *     position p = lens[r] - (off[r + 1] - t) of request r; its slot is
+ *     table[r, p / block] * block + p mod block.  Tokens from off[R] on are padding:
+ *     -1.  Requests may be empty; `off` must not decrease.  Reported: a position
+ *     outside the row or a negative block (the slot is -1 then).
+ * PUT_ROWS {dest[S, C], slots[T], rows[T, C]} -> dest with row slots[t] replaced by
+ *     rows[t].  Rows whose slot is negative are left out, and of several rows for
+ *     one slot the last one stays.  dest, rows and the result have one element
+ *     type, any of the five.  As for PERMUTE, every other use of dest must come in
+ *     an earlier cluster, because the result may be bound to dest's own buffer:
+ *     then only the rows that are put are touched; bound elsewhere, dest is copied
+ *     first.  Reported: a slot beyond S (the row is left out).
+ * PAGED_ATTENTION {q[B, Hq * D], keys[S, Hk * D], values[S, Hk * D], table[B, W], lens[B]} -> [B, Hq * D]
+ *     Row b attends to the tokens of request b: for head h, with K and V those of
+ *     head h / (Hq / Hk), the mean of V weighted with softmax(scale * q . K).
+ *     D = iparam[1] is a multiple of 8 up to 256, Hq a multiple of Hk.
+ *     scale = fparam[0].  iparam[2] > 0: only the last iparam[2] tokens (a sliding
+ *     window).  A request without tokens yields zeros.  One element type of F32,
+ *     F16, BF16; products, softmax and sums are held in 32 bits.  Reported: a
+ *     negative length (no tokens), a length beyond W * block (cut off), a block
+ *     outside the cache (its tokens are left out).
+ * PENALIZE {logits[B, V], tokens[B, L], params[B, 4], bias_ids[B, K], bias[B, K], mask[B, M]} -> [B, V]
+ *     params[b] = (repetition, frequency, presence, prompt), fp32.  With x the logit
+ *     of v in 32 bits, every operation rounded:
+ *       v among tokens[b]:  x = x > 0 ? x / repetition : x * repetition
+ *       c times among the entries of tokens[b] from number `prompt` on:
+ *                           x = x - frequency * c;  x = x - presence if c > 0
+ *       v among bias_ids[b]: x = x + the sum of its biases, added up in list order
+ *       M > 0 and bit v mod 32 of mask[b, v / 32] not set: x = -infinity
+ *     Negative tokens and ids are padding.  M is 0 (no mask) or ceil(V / 32).
+ *     Logits and result have one element type of F32, F16, BF16.  May be bound in
+ *     place of the logits.  Reported: a token or id beyond V (left out).
+ *
+ * An operator's result must not overlap its inputs in memory but for the cases
+ * named above (ACC_ERR_ARG from acc_run, acc_workspace_bytes); in place, every other
+ * reader of the overwritten array must run earlier (ACC_ERR_ILLEGAL_SCATTER). */
 
 /* ---- clustering (Sections 3.4, 4.1, 4.2; Figure 3) -------------------------- */
 

@@ -10,6 +10,7 @@ it; the CUDA library never calls it either.
   legality      the paper's legality model evaluated for a given clustering,
                 and the enumeration of every legal clustering
   functions     the element-level function tables
+  operators     foreign functions: paged caches, attention over them, logits
 
 Pins (see tests/test_oracle_*.py): hand-worked examples per combinator, closed
 forms, the equivalences and the printed loops of the paper, the printed graph
@@ -19,4 +20,4 @@ stream of the Zipf sampler in the input generator (only its range and its
 leading frequency are checked) -- "parity unpinned" for that generator, which
 is an input recipe and not part of the method.
 """
-from . import functions, interp, legality, cluster_loop  # noqa: F401
+from . import functions, operators, interp, legality, cluster_loop  # noqa: F401

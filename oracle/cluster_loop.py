@@ -17,6 +17,7 @@ programs.  fp32 accumulations are carried in fp64 as in the interpreter.
 import numpy as np
 
 from . import functions as fns
+from . import operators
 from .interp import to_internal, _np_dtype, _count, F32, F64, U32
 from .legality import edges_of, manifest_set
 
@@ -148,6 +149,8 @@ class _Cluster:
         n = _count(shape)
         dt = _np_dtype(nd.dtype)
         out = np.empty(n, dtype=dt)
+        if nd.kind in operators.KINDS:             # a cluster of its own: whole arrays in, a whole array out
+            return operators.evaluate(nd, [self.mem[s] for s in nd.inputs])
         if nd.kind == "permute":
             dest, ind, vals = nd.inputs[:3]
             acc = [float(v) if nd.dtype == "f32" else v for v in self.mem[dest].reshape(-1)]

@@ -24,12 +24,13 @@ Integers are uint32 bit patterns with wrap-around.
 import numpy as np
 
 from . import functions as fns
+from . import operators
 
 F32, F64, U32 = np.float32, np.float64, np.uint32
 
 
 def _np_dtype(dt):
-    return F32 if dt == "f32" else U32
+    return {"f32": F32, "f16": np.float16, "bf16": np.uint16}.get(dt, U32)
 
 
 def _count(shape):
@@ -45,6 +46,9 @@ def to_internal(arr, dtype):
     if dtype == "f32":
         assert a.dtype == F32
         return a
+    if dtype in ("f16", "bf16"):                 # (bf16: the patterns, as 16-bit integers)
+        assert a.dtype.itemsize == 2
+        return a.view(_np_dtype(dtype))
     assert a.dtype.itemsize == 4
     return a.view(U32)
 
@@ -69,8 +73,9 @@ class Result:
         self.values, self.exact, self.abs_sum = {}, {}, {}
 
 
-def run(nodes, inputs, stop_after=None):
-    """Evaluate nodes in order.  inputs: {node id: array}.  Returns a Result."""
+def run(nodes, inputs, stop_after=None, strict=True):
+    """Evaluate nodes in order.  inputs: {node id: array}.  Returns a Result.
+    strict=False: operators go on where the library goes on and reports a number outside its range."""
     res = Result()
     val = res.values
     for i, nd in enumerate(nodes):
@@ -117,6 +122,8 @@ def run(nodes, inputs, stop_after=None):
         elif k == "permute":
             dest, ind, vals = (val[s] for s in nd.inputs[:3])
             out = _permute(res, i, nd, dest, ind, vals).reshape(shape)
+        elif k in operators.KINDS:
+            out = operators.evaluate(nd, [val[s] for s in nd.inputs], res, i, strict)
         else:
             raise KeyError(k)
         val[i] = np.ascontiguousarray(out).reshape(shape)

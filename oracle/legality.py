@@ -9,8 +9,9 @@ numbers instead of being solved:
     forced by  x_ab <= pi_b - pi_a <= n * x_ab);
   * infusible edges: out of a program input; into a free-variable (indexed)
     slot; into the destination slot of a scatter and out of a scatter's
-    result; through force();
-  * a scatter comes strictly after every other consumer of its destination;
+    result; through force(); into and out of an operator (a foreign function);
+  * a scatter, and an operator that puts rows, comes strictly after every other
+    consumer of its destination;
   * an array is fused away (m_a = 1) only if all of its out-edges are fused
     and it is not a program output; otherwise it is manifest and its order
     d^o_a is 0 or 1;
@@ -44,6 +45,8 @@ parent that copies of two members read in the same order.
 """
 from itertools import product
 
+from .operators import KINDS as OPERATORS
+
 
 class Edge:
     __slots__ = ("a", "b", "slot", "fusible", "ordered")
@@ -62,8 +65,8 @@ def edges_of(nodes):
             dest = nd.kind == "permute" and s == 0
             forced = s in tuple(getattr(nd, "force", ()))
             from_scatter = pa.kind == "permute"
-            ordered = not (free or dest or forced or from_scatter)
-            fusible = ordered and pa.kind != "input"
+            ordered = not (free or dest or forced or from_scatter or nd.kind in OPERATORS)
+            fusible = ordered and pa.kind != "input" and pa.kind not in OPERATORS
             out.append(Edge(a, b, s, fusible, ordered))
     return out
 
@@ -129,7 +132,7 @@ def solve(nodes, outputs, pi, recompute=0):
         if not e.fusible and pi[e.a] == pi[e.b]:
             return False, f"infusible: edge {e.a}->{e.b} inside one cluster", None
     for j, nd in enumerate(nodes):
-        if nd.kind != "permute":
+        if nd.kind not in ("permute", "put_rows"):
             continue
         dest = nd.inputs[0]
         for e in edges:
@@ -321,7 +324,7 @@ def canonical_pi(nodes, blocks):
         if e.a in blk and blk[e.a] != blk[e.b]:
             before[blk[e.b]].add(blk[e.a])
     for j, nd in enumerate(nodes):
-        if nd.kind == "permute":
+        if nd.kind in ("permute", "put_rows"):
             for e in edges:
                 if e.a == nd.inputs[0] and e.b != j:
                     if blk[e.b] == blk[j]:

@@ -39,8 +39,10 @@ def _parse_enums(path):
 ENUM = _parse_enums(HEADER)
 KIND = {k[4:].lower(): v for k, v in ENUM.items()
         if k in ("ACC_INPUT", "ACC_GENERATE", "ACC_MAP", "ACC_ZIPWITH", "ACC_BACKPERMUTE", "ACC_GATHER",
-                 "ACC_PERMUTE", "ACC_FOLD", "ACC_FOLDSEG", "ACC_SCANL", "ACC_SCANR")}
-DTYPE = {"f32": ENUM["ACC_F32"], "i32": ENUM["ACC_I32"], "u32": ENUM["ACC_U32"]}
+                 "ACC_PERMUTE", "ACC_FOLD", "ACC_FOLDSEG", "ACC_SCANL", "ACC_SCANR", "ACC_BLOCK_TABLE", "ACC_SLOT_MAP",
+                 "ACC_PUT_ROWS", "ACC_PAGED_ATTENTION", "ACC_PENALIZE")}
+DTYPE = {k: ENUM["ACC_" + k.upper()] for k in ("f32", "i32", "u32", "f16", "bf16")}
+_HALF = (DTYPE["f16"], DTYPE["bf16"])
 FN = {k[7:].lower(): v for k, v in ENUM.items() if k.startswith("ACC_FN_")}
 IDX_FN = {k[8:].lower(): v for k, v in ENUM.items() if k.startswith("ACC_IDX_")}
 STATUS_NAME = {v: k for k, v in ENUM.items() if k.startswith("ACC_ERR_") or k == "ACC_OK"}
@@ -185,6 +187,7 @@ class Graph:
         self._h = C.c_void_p()
         _check(lib().acc_graph_create(C.byref(self._h)))
         self._keep = {}          # tensors bound to nodes stay alive with the graph
+        self._size = []          # bytes of an element, by node
         self.workspace = None
         if nodes is not None:
             for nd in nodes:
@@ -206,7 +209,12 @@ class Graph:
     # ---- graph ------------------------------------------------------------------
     def add_node(self, nd):
         d = nd if isinstance(nd, NodeDesc) else make_desc(nd)
-        return _check(lib().acc_add_node(self._h, C.byref(d)))
+        node = _check(lib().acc_add_node(self._h, C.byref(d)))
+        self._size.append(2 if d.dtype in _HALF else 4)
+        return node
+
+    def _fits(self, n, tensor):
+        return not 0 <= n < len(self._size) or tensor.element_size() == self._size[n]    # (the library knows which nodes there are)
 
     def mark_output(self, n):
         _check(lib().acc_mark_output(self._h, n))
@@ -301,14 +309,14 @@ class Graph:
 
     # ---- running ----------------------------------------------------------------
     def bind(self, n, tensor):
-        """Binds a CUDA tensor (4-byte elements, contiguous) to node n."""
-        assert tensor.is_cuda and tensor.is_contiguous() and tensor.element_size() == 4
-        _check(lib().acc_bind(self._h, n, C.c_void_p(tensor.data_ptr()), tensor.numel() * 4))
+        """Binds a CUDA tensor (elements of the node's size, contiguous) to node n."""
+        assert tensor.is_cuda and tensor.is_contiguous() and self._fits(n, tensor)
+        _check(lib().acc_bind(self._h, n, C.c_void_p(tensor.data_ptr()), tensor.numel() * tensor.element_size()))
         self._keep[("dev", n)] = tensor
 
     def bind_host(self, n, tensor):
-        assert not tensor.is_cuda and tensor.is_contiguous() and tensor.element_size() == 4
-        _check(lib().acc_bind_host(self._h, n, C.c_void_p(tensor.data_ptr()), tensor.numel() * 4))
+        assert not tensor.is_cuda and tensor.is_contiguous() and self._fits(n, tensor)
+        _check(lib().acc_bind_host(self._h, n, C.c_void_p(tensor.data_ptr()), tensor.numel() * tensor.element_size()))
         self._keep[("host", n)] = tensor
 
     def workspace_bytes(self, executor=FUSED):

@@ -273,7 +273,7 @@ int acc_bind(acc_graph* g, acc_node n, void* device_ptr, size_t bytes) {
   clear_error();
   if (!g || bad_node(g, n)) return set_error(ACC_ERR_ARG, "bad node id");
   Node& nd = g->nodes[n];
-  if (bytes < (size_t)nd.count * 4) return set_error(ACC_ERR_UNBOUND, "node %d needs %zu bytes, buffer has %zu", n, (size_t)nd.count * 4, bytes);
+  if (bytes < array_bytes(nd)) return set_error(ACC_ERR_UNBOUND, "node %d needs %zu bytes, buffer has %zu", n, array_bytes(nd), bytes);
   if (!device_ptr && nd.count > 0) return set_error(ACC_ERR_ARG, "device pointer is null");
   if (reinterpret_cast<uintptr_t>(device_ptr) & 15) return set_error(ACC_ERR_ARG, "device pointer is not 16-byte aligned");
   nd.dev = device_ptr;
@@ -287,7 +287,7 @@ int acc_bind_host(acc_graph* g, acc_node n, void* host_ptr, size_t bytes) {
   if (!g || bad_node(g, n)) return set_error(ACC_ERR_ARG, "bad node id");
   Node& nd = g->nodes[n];
   if (!is_input(nd) && !nd.output) return set_error(ACC_ERR_ARG, "node %d is neither an input nor a marked output", n);
-  if (bytes < (size_t)nd.count * 4 || (!host_ptr && nd.count > 0)) return set_error(ACC_ERR_UNBOUND, "host buffer of node %d is null or too small", n);
+  if (bytes < array_bytes(nd) || (!host_ptr && nd.count > 0)) return set_error(ACC_ERR_UNBOUND, "host buffer of node %d is null or too small", n);
   nd.host = host_ptr;
   nd.host_bytes = bytes;
   return ACC_OK;
@@ -372,7 +372,7 @@ int acc_run_e2e_async(acc_graph* g, void* workspace, size_t workspace_bytes, voi
   for (Node& nd : g->nodes)
     if (is_input(nd) && nd.host) {
       if (!nd.dev) return set_error(ACC_ERR_UNBOUND, "a host-bound input has no device buffer");
-      const size_t b = (size_t)nd.count * 4;
+      const size_t b = array_bytes(nd);
       if (b && cudaMemcpyAsync(nd.dev, nd.host, b, cudaMemcpyHostToDevice, stream) != cudaSuccess)
         return set_error(ACC_ERR_CUDA, "host-to-device copy failed: %s", cudaGetErrorString(cudaGetLastError()));
       up += b;
@@ -381,7 +381,7 @@ int acc_run_e2e_async(acc_graph* g, void* workspace, size_t workspace_bytes, voi
   if (rc != ACC_OK) return rc;
   for (Node& nd : g->nodes)
     if (nd.output && nd.host) {
-      const size_t b = (size_t)nd.count * 4;
+      const size_t b = array_bytes(nd);
       if (b && cudaMemcpyAsync(nd.host, nd.dev, b, cudaMemcpyDeviceToHost, stream) != cudaSuccess)
         return set_error(ACC_ERR_CUDA, "device-to-host copy failed: %s", cudaGetErrorString(cudaGetLastError()));
       down += b;

@@ -83,6 +83,10 @@ static dev::NodeArg node_arg(const Node& n, const void* ptr) {
 
 // The kernel instantiated for a cluster: for its very constants, else the one that takes them at run time.
 static const KernelEntry* lookup(CCluster& cc, std::string& sig) {
+  if (cc.n > 0 && is_operator(cc.nodes[cc.n - 1].kind)) {   // (alone in its cluster, behind its inputs)
+    sig = operator_signature(cc.nodes[cc.n - 1].kind);
+    return find_kernel(sig);
+  }
   sig = signature(cc);
   const KernelEntry* k = find_kernel(sig);
   if (!k) {
@@ -137,6 +141,27 @@ int refine_to_kernels(const Graph& g, std::vector<int32_t>& pi, int recompute_de
   }
 }
 
+// An operator's result lies apart from its inputs, or exactly on the one that it may replace; what it replaces is read by
+// nobody who runs later.  (Results in the workspace have places of their own.)
+static int check_operator_buffers(const Graph& g, const std::vector<int32_t>& pi, int node) {
+  const Node& nd = g.nodes[node];
+  const int kind = nd.d.kind;
+  const int replaced = kind == ACC_PUT_ROWS || kind == ACC_PENALIZE ? 0 : kind == ACC_BLOCK_TABLE && nd.d.n_inputs == 4 ? 3 : -1;
+  if (!nd.dev || array_bytes(nd) == 0) return ACC_OK;
+  const uintptr_t lo = reinterpret_cast<uintptr_t>(nd.dev), hi = lo + array_bytes(nd);
+  for (int s = 0; s < nd.d.n_inputs; ++s) {
+    const int a = nd.d.inputs[s];
+    const Node& from = g.nodes[a];
+    const uintptr_t p = reinterpret_cast<uintptr_t>(from.dev);
+    if (!from.dev || p >= hi || p + array_bytes(from) <= lo) continue;
+    if (s != replaced || p != lo) return set_error(ACC_ERR_ARG, "node %d: its buffer overlaps that of its slot %d (node %d)", node, s, a);
+    for (const Edge& e : g.edges)
+      if (e.a == a && !(e.b == node ? e.slot == s : pi[e.b] < pi[node]))
+        return set_error(ACC_ERR_ILLEGAL_SCATTER, "node %d overwrites node %d, which node %d does not read earlier", node, a, e.b);
+  }
+  return ACC_OK;
+}
+
 int build_schedule(Graph& g, int executor, Schedule& sch) {
   const int n = (int)g.nodes.size();
   sch = Schedule{};
@@ -167,7 +192,7 @@ int build_schedule(Graph& g, int executor, Schedule& sch) {
     }
     if (!man[i] || nd.dev) continue;
     sch.array_off[i] = off;
-    off += align_up((size_t)std::max<int64_t>(nd.count, 1) * 4, 256);
+    off += align_up(std::max<size_t>(array_bytes(nd), 4), 256);
   }
   sch.array_bytes = off;
 
@@ -188,6 +213,17 @@ int build_schedule(Graph& g, int executor, Schedule& sch) {
                        st.n_members, st.first_node, sig.c_str());
     st.launch.n = st.cc.n;
     for (int li = 0; li < st.cc.n; ++li) st.launch.nodes[li] = node_arg(g.nodes[st.cc.source[li]], nullptr);
+    if (is_operator(st.cc.nodes[st.cc.n - 1].kind)) {
+      const CNode& op = st.cc.nodes[st.cc.n - 1];
+      st.launch.op = g.nodes[st.first_node].d;
+      st.launch.result = st.cc.n - 1;
+      for (int s = 0; s < op.nin; ++s) {
+        st.launch.slot[s] = op.in[s];
+        st.launch.slot_dtype[s] = st.cc.nodes[op.in[s]].dtype;
+      }
+      const int rc = check_operator_buffers(g, pi, st.first_node);
+      if (rc != ACC_OK) return rc;
+    }
     const int64_t sb = st.kernel->scratch_bytes(st.launch);
     if (sb < 0) return set_error((int)sb, "cluster at node %d: no scratch layout", st.first_node);
     const int64_t zb = st.kernel->zeroed_bytes(st.launch);
@@ -432,7 +468,7 @@ int finish(Graph& g, void* workspace, cudaStream_t stream) {
   const volatile uint32_t* words = r.words.get();
   const auto raised = [&](int condition) { return r.captured ? words[condition] != 0 : words[condition] == r.run_id; };
   if (raised(dev::kStatusTimeout)) return set_error(ACC_ERR_DEVICE_TIMEOUT, "a device-side wait ran out of iterations");
-  if (raised(dev::kStatusIndex)) return set_error(ACC_ERR_INDEX_RANGE, "a scatter index or a segment offset fell outside its array");
+  if (raised(dev::kStatusIndex)) return set_error(ACC_ERR_INDEX_RANGE, "a scatter index, a segment offset or a number that an operator was given fell outside its array");
   if (raised(dev::kStatusEmptySegment)) return set_error(ACC_ERR_SHAPE, "an empty segment has no value: segment offsets must increase");
   std::lock_guard<std::mutex> lock(g.reports_guard);
   const RunReport* now = report_for(g, workspace);

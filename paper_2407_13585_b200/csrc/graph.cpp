@@ -62,10 +62,78 @@ static int fn_domain(int fn) {
   }
 }
 
+// An operator's slots, shapes, types and constants.
+static int check_operator(const Graph& g, const acc_node_desc& d, int id) {
+  auto in = [&](int s) -> const acc_node_desc& { return g.nodes[d.inputs[s]].d; };
+  auto is_shape = [](const acc_node_desc& a, int64_t rows, int64_t cols) { return a.rank == 2 && a.shape[0] == rows && a.shape[1] == cols; };
+  auto is_rank1 = [](const acc_node_desc& a, int64_t n) { return a.rank == 1 && a.shape[0] == n; };
+  auto is_real = [](int dt) { return dt == ACC_F32 || is_half(dt); };
+  const int n = d.n_inputs;
+  const int want = d.kind == ACC_BLOCK_TABLE ? (n == 4 ? 4 : 2) : d.kind == ACC_PAGED_ATTENTION ? 5 : d.kind == ACC_PENALIZE ? 6 : 3;
+  if (n != want || d.n_array_inputs != n) return set_error(ACC_ERR_ARG, "node %d: the operator takes %d array slots and no free ones", id, want);
+  if (d.fn_id || d.idx_fn_id) return set_error(ACC_ERR_ARG, "node %d: an operator has no element function", id);
+  const bool paged = d.kind == ACC_BLOCK_TABLE || d.kind == ACC_SLOT_MAP || d.kind == ACC_PAGED_ATTENTION;
+  if (paged && (d.iparam[0] < 1 || d.iparam[0] > ACC_MAX_ELEMENTS)) return set_error(ACC_ERR_ARG, "node %d: blocks of %lld slots", id, (long long)d.iparam[0]);
+  auto integers = [&](int s) -> int {
+    return is_int(in(s).dtype) ? ACC_OK : set_error(ACC_ERR_DTYPE, "node %d: slot %d must be integer", id, s);
+  };
+  int rc = ACC_OK;
+  switch (d.kind) {
+    case ACC_BLOCK_TABLE:
+      for (int s = 0; s < n && rc == ACC_OK; ++s) rc = integers(s);
+      if (rc != ACC_OK) return rc;
+      if (!is_int(d.dtype)) return set_error(ACC_ERR_DTYPE, "node %d: a table holds integers", id);
+      if (d.rank != 2 || !is_rank1(in(0), d.shape[0]) || in(1).rank != 1) return set_error(ACC_ERR_SHAPE, "node %d: R lengths and a list give R rows", id);
+      if (n == 4 && (!is_rank1(in(2), d.shape[0]) || !is_shape(in(3), d.shape[0], d.shape[1])))
+        return set_error(ACC_ERR_SHAPE, "node %d: the old table must have the new one's shape", id);
+      return ACC_OK;
+    case ACC_SLOT_MAP:
+      for (int s = 0; s < n && rc == ACC_OK; ++s) rc = integers(s);
+      if (rc != ACC_OK) return rc;
+      if (!is_int(d.dtype)) return set_error(ACC_ERR_DTYPE, "node %d: slots are integers", id);
+      if (d.rank != 1 || in(0).rank != 2 || !is_rank1(in(1), in(0).shape[0]) || !is_rank1(in(2), in(0).shape[0] + 1))
+        return set_error(ACC_ERR_SHAPE, "node %d: a table of R rows needs R lengths and R+1 offsets", id);
+      return ACC_OK;
+    case ACC_PUT_ROWS:
+      if ((rc = integers(1)) != ACC_OK) return rc;
+      if (in(0).dtype != d.dtype || in(2).dtype != d.dtype) return set_error(ACC_ERR_DTYPE, "node %d: destination, rows and result differ in type", id);
+      if (d.rank != 2 || !same_shape(in(0), d)) return set_error(ACC_ERR_SHAPE, "node %d: the result has the destination's shape, rank 2", id);
+      if (in(1).rank != 1 || !is_shape(in(2), in(1).shape[0], d.shape[1])) return set_error(ACC_ERR_SHAPE, "node %d: T slots need T rows of the destination's width", id);
+      return ACC_OK;
+    case ACC_PAGED_ATTENTION: {
+      if ((rc = integers(3)) != ACC_OK || (rc = integers(4)) != ACC_OK) return rc;
+      for (int s = 0; s < 3; ++s)
+        if (!is_real(d.dtype) || in(s).dtype != d.dtype) return set_error(ACC_ERR_DTYPE, "node %d: queries, keys, values and result must have one type of f32, f16, bf16", id);
+      const int64_t D = d.iparam[1];
+      if (D < 8 || D > 256 || D % 8) return set_error(ACC_ERR_UNSUPPORTED, "node %d: heads of %lld elements; built for multiples of 8 up to 256", id, (long long)D);
+      if (d.iparam[2] < 0) return set_error(ACC_ERR_ARG, "node %d: negative window", id);
+      if (d.rank != 2 || !same_shape(in(0), d)) return set_error(ACC_ERR_SHAPE, "node %d: the result has the queries' shape, rank 2", id);
+      if (in(1).rank != 2 || !same_shape(in(1), in(2))) return set_error(ACC_ERR_SHAPE, "node %d: keys and values have one shape, rank 2", id);
+      if (d.shape[1] % D || in(1).shape[1] % D) return set_error(ACC_ERR_SHAPE, "node %d: rows are not made of heads of %lld", id, (long long)D);
+      const int64_t hq = d.shape[1] / D, hk = in(1).shape[1] / D;
+      if (hq > 0 && (hk < 1 || hq % hk)) return set_error(ACC_ERR_SHAPE, "node %d: %lld query heads over %lld key heads", id, (long long)hq, (long long)hk);
+      if (in(3).rank != 2 || in(3).shape[0] != d.shape[0] || !is_rank1(in(4), d.shape[0]))
+        return set_error(ACC_ERR_SHAPE, "node %d: B rows need a table of B rows and B lengths", id);
+      return ACC_OK;
+    }
+    default: {                                             // ACC_PENALIZE
+      if ((rc = integers(1)) != ACC_OK || (rc = integers(3)) != ACC_OK || (rc = integers(5)) != ACC_OK) return rc;
+      if (!is_real(d.dtype) || in(0).dtype != d.dtype) return set_error(ACC_ERR_DTYPE, "node %d: logits and result must have one type of f32, f16, bf16", id);
+      if (in(2).dtype != ACC_F32 || in(4).dtype != ACC_F32) return set_error(ACC_ERR_DTYPE, "node %d: parameters and biases are fp32", id);
+      if (d.rank != 2 || !same_shape(in(0), d)) return set_error(ACC_ERR_SHAPE, "node %d: the result has the logits' shape, rank 2", id);
+      const int64_t B = d.shape[0], words = (d.shape[1] + 31) / 32;
+      if (in(1).rank != 2 || in(1).shape[0] != B || !is_shape(in(2), B, 4) || in(3).rank != 2 || in(3).shape[0] != B || !same_shape(in(3), in(4)))
+        return set_error(ACC_ERR_SHAPE, "node %d: tokens, 4 parameters, ids and biases for every row", id);
+      if (!is_shape(in(5), B, 0) && !is_shape(in(5), B, words)) return set_error(ACC_ERR_SHAPE, "node %d: the mask has 0 or %lld words a row", id, (long long)words);
+      return ACC_OK;
+    }
+  }
+}
+
 int add_node(Graph& g, const acc_node_desc& d) {
   const int id = (int)g.nodes.size();
-  if (d.kind < ACC_INPUT || d.kind > ACC_SCANR) return set_error(ACC_ERR_ARG, "node %d: unknown kind %d", id, d.kind);
-  if (d.dtype < ACC_F32 || d.dtype > ACC_U32) return set_error(ACC_ERR_DTYPE, "node %d: unknown dtype %d", id, d.dtype);
+  if (d.kind < ACC_INPUT || d.kind > ACC_PENALIZE) return set_error(ACC_ERR_ARG, "node %d: unknown kind %d", id, d.kind);
+  if (d.dtype < ACC_F32 || d.dtype > ACC_BF16) return set_error(ACC_ERR_DTYPE, "node %d: unknown dtype %d", id, d.dtype);
   if (d.rank < 0 || d.rank > 2) return set_error(ACC_ERR_SHAPE, "node %d: rank %d outside 0..2", id, d.rank);
   int64_t count = 1;
   for (int i = 0; i < d.rank; ++i) {
@@ -82,6 +150,11 @@ int add_node(Graph& g, const acc_node_desc& d) {
     if (d.inputs[s] < 0 || d.inputs[s] >= id) return set_error(ACC_ERR_ARG, "node %d: slot %d names node %d", id, s, d.inputs[s]);
   auto in = [&](int s) -> const acc_node_desc& { return g.nodes[d.inputs[s]].d; };
   const int n_free = d.n_inputs - d.n_array_inputs;
+  if (d.kind != ACC_INPUT && !is_operator(d.kind)) {       // the combinators' code is that of 4-byte elements
+    if (is_half(d.dtype)) return set_error(ACC_ERR_DTYPE, "node %d: a combinator has 4-byte elements", id);
+    for (int s = 0; s < d.n_inputs; ++s)
+      if (is_half(in(s).dtype)) return set_error(ACC_ERR_DTYPE, "node %d: slot %d has 2-byte elements, which only operators read", id, s);
+  }
 
   switch (d.kind) {
     case ACC_INPUT:
@@ -196,6 +269,10 @@ int add_node(Graph& g, const acc_node_desc& d) {
       if (in(0).dtype != d.dtype) return set_error(ACC_ERR_DTYPE, "node %d: dtype differs from its source", id);
       break;
     }
+    default: {
+      const int rc = check_operator(g, d, id);
+      if (rc != ACC_OK) return rc;
+    }
   }
   for (int s = d.n_array_inputs; s < d.n_inputs; ++s)
     if (g.nodes[d.inputs[s]].count < 1) return set_error(ACC_ERR_SHAPE, "node %d: free variable %d is empty", id, s);
@@ -214,8 +291,8 @@ int add_node(Graph& g, const acc_node_desc& d) {
     e.a = d.inputs[s];
     e.b = id;
     e.slot = s;
-    e.ordered = !(free_slot || dest || forced || from_scatter);
-    e.fusible = e.ordered && !is_input(p);
+    e.ordered = !(free_slot || dest || forced || from_scatter || is_operator(d.kind));
+    e.fusible = e.ordered && !is_input(p) && !is_operator(p.d.kind);
     g.edges.push_back(e);
   }
   g.has_pi = false;

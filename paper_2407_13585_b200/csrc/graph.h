@@ -63,6 +63,13 @@ struct Graph {
 };
 
 inline bool is_input(const Node& n) { return n.d.kind == ACC_INPUT; }
+// A node kind that one kernel of its own computes (a foreign function, Section 3.4): all its edges are infusible.
+constexpr bool is_operator(int kind) { return kind >= ACC_BLOCK_TABLE && kind <= ACC_PENALIZE; }
+// Nodes that overwrite an array: other uses of it come strictly earlier.
+constexpr bool overwrites_destination(int kind) { return kind == ACC_PERMUTE || kind == ACC_PUT_ROWS; }
+constexpr bool is_half(int dtype) { return dtype == ACC_F16 || dtype == ACC_BF16; }
+constexpr size_t element_bytes(int dtype) { return is_half(dtype) ? 2 : 4; }
+inline size_t array_bytes(const Node& n) { return (size_t)n.count * element_bytes(n.d.dtype); }
 inline bool gather_like(const Node& n) { return n.d.kind == ACC_GATHER || n.d.kind == ACC_BACKPERMUTE; }
 
 int  set_error(int code, const char* fmt, ...);

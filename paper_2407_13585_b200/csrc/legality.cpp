@@ -260,7 +260,7 @@ bool partial_clustering_possible(const Graph& g, const std::vector<int>& block_o
     else link(block_of[e.a], block_of[e.b]);
   }
   for (int j = 0; j < n; ++j) {
-    if (g.nodes[j].d.kind != ACC_PERMUTE || block_of[j] < 0) continue;
+    if (!overwrites_destination(g.nodes[j].d.kind) || block_of[j] < 0) continue;
     const int dest = g.nodes[j].d.inputs[0];
     for (const Edge& e : g.edges)
       if (e.a == dest && e.b != j && block_of[e.b] >= 0) {
@@ -336,7 +336,7 @@ int check_partition(const Graph& g, const int32_t* pi, Solution* sol, bool quiet
     if (!e.fusible && pi[e.a] == pi[e.b]) return fail(ACC_ERR_ILLEGAL_INFUSIBLE, "infusible edge inside one cluster", e.a, e.b);
   }
   for (int j = 0; j < n; ++j) {
-    if (g.nodes[j].d.kind != ACC_PERMUTE) continue;
+    if (!overwrites_destination(g.nodes[j].d.kind)) continue;
     const int dest = g.nodes[j].d.inputs[0];
     for (const Edge& e : g.edges)
       if (e.a == dest && e.b != j && !(pi[e.b] < pi[j]))

@@ -1,0 +1,88 @@
+// What the operators (foreign functions, Section 3.4) share: how a launch finds its slots, element types, status words.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <atomic>
+#include <cstdint>
+
+#include "acc.h"
+#include "device/eval.cuh"
+#include "graph.h"
+#include "registry.h"
+
+namespace acc {
+namespace ops {
+
+// Where a kernel reports to (see raise_status in device/eval.cuh); the first member of every operator's parameters.
+struct Report {
+  uint32_t* status;
+  uint32_t run_id;
+};
+inline Report report_of(const ClusterLaunch& L) { return {L.status, L.run_id}; }
+__device__ __forceinline__ void raise_index(const Report& r) { *reinterpret_cast<volatile uint32_t*>(r.status + dev::kStatusIndex) = r.run_id; }
+
+inline const dev::NodeArg& slot(const ClusterLaunch& L, int s) { return L.nodes[L.slot[s]]; }
+template <class T>
+const T* slot_ptr(const ClusterLaunch& L, int s) { return static_cast<const T*>(slot(L, s).ptr); }
+template <class T>
+T* result_ptr(const ClusterLaunch& L) { return static_cast<T*>(const_cast<void*>(L.nodes[L.result].ptr)); }
+
+// Unsigned division by a constant of the launch: dev::div_by with the multiplier of dev::NodeArg.
+struct Divisor {
+  uint32_t d, mul, sh1, sh2;
+};
+inline Divisor divisor(uint32_t d) {
+  uint32_t l = 0;
+  while (l < 32 && (1ull << l) < d) ++l;
+  const uint32_t sh1 = l < 1 ? l : 1;
+  return {d, (uint32_t)((((1ull << l) - d) << 32) / d + 1), sh1, l - sh1};
+}
+__device__ __forceinline__ uint32_t operator/(uint32_t v, const Divisor& p) {
+  const uint32_t t = __umulhi(v, p.mul);
+  return (t + ((v - t) >> p.sh1)) >> p.sh2;
+}
+
+// The blocks that `length` tokens take up.
+__device__ __forceinline__ int blocks_of(int length, const Divisor& block) { return length <= 0 ? 0 : (int)((uint32_t)(length - 1) / block) + 1; }
+
+inline int launched() {
+  const cudaError_t e = cudaGetLastError();
+  return e == cudaSuccess ? ACC_OK : set_error(ACC_ERR_CUDA, "kernel launch failed: %s", cudaGetErrorString(e));
+}
+
+// Lets a kernel have `bytes` of dynamic shared memory on the current device (asked for once per device and kernel).
+template <class K>
+int allow_shared(K kernel, size_t bytes, std::atomic<uint64_t>& devices) {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return set_error(ACC_ERR_CUDA, "no current device: %s", cudaGetErrorString(cudaGetLastError()));
+  const uint64_t bit = 1ull << (dev & 63);
+  if (dev < 64 && (devices.load(std::memory_order_relaxed) & bit)) return ACC_OK;
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+  if (e != cudaSuccess) return set_error(ACC_ERR_CUDA, "%zu bytes of shared memory: %s", bytes, cudaGetErrorString(cudaGetLastError()));
+  devices.fetch_or(bit, std::memory_order_relaxed);
+  return ACC_OK;
+}
+
+inline int64_t no_scratch(const ClusterLaunch&) { return 0; }
+
+struct Register {
+  Register(int kind, const char* name, int64_t (*scratch)(const ClusterLaunch&), int (*launch)(const ClusterLaunch&)) {
+    register_kernel(KernelEntry{operator_signature(kind), name, scratch, no_scratch, launch, 1});
+  }
+};
+
+template <class T> __device__ __forceinline__ float widen(T x);
+template <> __device__ __forceinline__ float widen<float>(float x) { return x; }
+template <> __device__ __forceinline__ float widen<__half>(__half x) { return __half2float(x); }
+template <> __device__ __forceinline__ float widen<__nv_bfloat16>(__nv_bfloat16 x) { return __bfloat162float(x); }
+// One rounding, to nearest even; beyond the type's range an infinity.
+template <class T> __device__ __forceinline__ T narrow(float x);
+template <> __device__ __forceinline__ float narrow<float>(float x) { return x; }
+template <> __device__ __forceinline__ __half narrow<__half>(float x) { return __float2half_rn(x); }
+template <> __device__ __forceinline__ __nv_bfloat16 narrow<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
+
+}  // namespace ops
+}  // namespace acc

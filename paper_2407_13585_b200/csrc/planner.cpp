@@ -24,7 +24,7 @@ bool canonical_numbering(const Graph& g, const std::vector<int>& block_of, int n
     if (block_of[e.a] != block_of[e.b]) before[block_of[e.b]].insert(block_of[e.a]);
   }
   for (int j = 0; j < n; ++j) {
-    if (g.nodes[j].d.kind != ACC_PERMUTE) continue;
+    if (!overwrites_destination(g.nodes[j].d.kind)) continue;
     const int dest = g.nodes[j].d.inputs[0];
     for (const Edge& e : g.edges)
       if (e.a == dest && e.b != j) {
@@ -55,7 +55,7 @@ int partition_cost(const Graph& g, const int32_t* pi, int cost, double* out, int
   const int rc = check_partition(g, pi, &sol, false, recompute_depth);
   if (rc != ACC_OK) return rc;
   const int n = (int)g.nodes.size();
-  auto bytes = [&](int a) { return double(std::max<int64_t>(g.nodes[a].count, 1)) * 4.0; };
+  auto bytes = [&](int a) { return double(std::max<int64_t>(g.nodes[a].count, 1)) * (double)element_bytes(g.nodes[a].d.dtype); };
   std::set<int> clusters;
   for (int i = 0; i < n; ++i)
     if (!is_input(g.nodes[i])) clusters.insert(pi[i]);
@@ -241,7 +241,7 @@ struct BranchBound {
       if (!e.fusible) apart[(size_t)e.a * n + e.b] = apart[(size_t)e.b * n + e.a] = 1;
   }
 
-  double weight(int a) const { return cost == ACC_COST_BYTES ? double(std::max<int64_t>(g.nodes[a].count, 1)) * 4.0 : 1.0; }
+  double weight(int a) const { return cost == ACC_COST_BYTES ? double(std::max<int64_t>(g.nodes[a].count, 1)) * (double)element_bytes(g.nodes[a].d.dtype) : 1.0; }
 
   // arrays that are manifest whatever happens to the nodes not placed yet
   void certain_manifest(std::vector<uint8_t>& man) const {

@@ -21,6 +21,8 @@ const KernelEntry* find_kernel(const std::string& sig) {
   return it == table().end() ? nullptr : &it->second;
 }
 
+std::string operator_signature(int kind) { return "O" + std::to_string(kind); }
+
 int registry_size() { return (int)table().size(); }
 
 int sm_count() {

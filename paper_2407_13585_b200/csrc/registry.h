@@ -20,6 +20,10 @@ struct ClusterLaunch {
   uint32_t run_id = 0;
   uint32_t spin_limit = 1u << 22;
   cudaStream_t stream = nullptr;
+  // An operator (graph.h, is_operator): its description, the local ids of its slots and of its result, their types
+  acc_node_desc op{};
+  int slot[kMaxSlots] = {}, result = 0;
+  int slot_dtype[kMaxSlots] = {};
   mutable int extra_launches = 0;   // set by a launcher that took more launches than its entry's `passes` (data-dependent paths)
 };
 
@@ -34,6 +38,8 @@ struct KernelEntry {
 
 void register_kernel(const KernelEntry& e);
 const KernelEntry* find_kernel(const std::string& sig);
+// The key of an operator's entry: its kind, whatever the types, slots and shapes (its launcher chooses among its kernels).
+std::string operator_signature(int kind);
 int registry_size();
 int sm_count();
 bool cooperative_launch_ok();   // the current device can run a grid with all blocks resident

@@ -12,7 +12,8 @@ the library's own legality checker), plus every node alone.
 
 Clusters the kernel skeletons cannot express are skipped and listed in a comment: a
 scan whose values are consumed inside its own cluster other than element for element, and a fold
-that is both written to memory and consumed inside its own cluster.
+that is both written to memory and consumed inside its own cluster.  Operators (foreign functions)
+need no instantiation: the clusters listed are those of the combinators around them.
 """
 import importlib
 import sys
@@ -21,8 +22,10 @@ from . import binding as B
 
 _KIND = {"foldseg": "ACC_FOLDSEG", "input": "ACC_INPUT", "generate": "ACC_GENERATE", "map": "ACC_MAP", "zipwith": "ACC_ZIPWITH",
          "backpermute": "ACC_BACKPERMUTE", "gather": "ACC_GATHER", "permute": "ACC_PERMUTE", "fold": "ACC_FOLD",
-         "scanl": "ACC_SCANL", "scanr": "ACC_SCANR"}
-_DT = {"f32": "ACC_F32", "i32": "ACC_I32", "u32": "ACC_U32"}
+         "scanl": "ACC_SCANL", "scanr": "ACC_SCANR", "block_table": "ACC_BLOCK_TABLE", "slot_map": "ACC_SLOT_MAP",
+         "put_rows": "ACC_PUT_ROWS", "paged_attention": "ACC_PAGED_ATTENTION", "penalize": "ACC_PENALIZE"}
+_DT = {"f32": "ACC_F32", "i32": "ACC_I32", "u32": "ACC_U32", "f16": "ACC_F16", "bf16": "ACC_BF16"}
+_OPERATORS = ("block_table", "slot_map", "put_rows", "paged_attention", "penalize")     # have kernels of their own
 
 
 def clusters_of(prog):
@@ -108,6 +111,8 @@ def emit(prog, out):
     out.write("  return p;\n}\ninline constexpr CProgram k_%s = make_%s();\n" % (name, name))
     skipped = []
     for members in clusters_of(prog):
+        if any(prog.nodes[i].kind in _OPERATORS for i in members):
+            continue
         mask = sum(1 << i for i in members)
         tag = "_".join(prog.nodes[i].name or str(i) for i in sorted(members))
         if expressible(prog, members):

@@ -1,0 +1,809 @@
+"""Operators (foreign functions: arrays that one kernel of their own computes): what the library accepts and refuses, how they
+sit in clusterings, the oracle's definitions worked by hand (no GPU needed), and the kernels against the oracle's loops in 64 bits."""
+import dataclasses
+
+import numpy as np
+import pytest
+
+import workloads as W
+from oracle import interp, legality as L, operators as O
+from paper_2407_13585_b200 import binding as B
+from workloads import Node
+
+REAL = ("f32", "f16", "bf16")
+EPS = {"f32": 2.0 ** -23, "f16": 2.0 ** -10, "bf16": 2.0 ** -7}
+TINY = {"f32": 2.0 ** -149, "f16": 2.0 ** -25, "bf16": 2.0 ** -133}     # half the smallest step (f32: a whole one)
+
+
+# ---- values of every type, as numpy arrays the oracle takes and as CUDA tensors -------------------------------
+
+def to_type(x, dtype):
+    return O.narrow(np.asarray(x, np.float64), dtype)
+
+
+def to_cuda(a, dtype):
+    import torch
+    if dtype == "bf16":
+        return torch.from_numpy(np.ascontiguousarray(a).view(np.int16)).view(torch.bfloat16).cuda()
+    if dtype in ("i32", "u32"):
+        return torch.from_numpy(np.ascontiguousarray(a).view(np.int32)).cuda()
+    return torch.from_numpy(np.ascontiguousarray(a)).cuda()
+
+
+def from_cuda(t, dtype):
+    import torch
+    if dtype == "bf16":
+        return t.view(torch.int16).cpu().numpy().view(np.uint16)
+    a = t.cpu().numpy()
+    return a.view(np.uint32) if dtype in ("i32", "u32") else a
+
+
+TORCH = {"f32": "float32", "f16": "float16", "bf16": "bfloat16", "i32": "int32", "u32": "int32"}
+
+
+class Bound:
+    """A program with its buffers: inputs by name, results filled with a pattern, or in place of an input."""
+
+    def __init__(self, prog, inputs, into=None, plan=True):
+        import torch
+        self.prog, self.g = prog, B.Graph(prog.nodes, prog.outputs)
+        if plan:
+            self.g.plan("branch_bound" if len(prog.nodes) > 14 else "enumerate", "bytes")
+        self.t = {}
+        for i in prog.input_ids():
+            nd = prog.nodes[i]
+            self.t[nd.name] = to_cuda(np.asarray(inputs[nd.name]).reshape(nd.shape), nd.dtype)
+            self.g.bind(i, self.t[nd.name])
+        for o in prog.outputs:
+            nd = prog.nodes[o]
+            if into and nd.name in into:
+                self.t[nd.name] = self.t[into[nd.name]]
+            else:
+                self.t[nd.name] = torch.full(nd.shape, 77, dtype=getattr(torch, TORCH[nd.dtype]), device="cuda")
+            self.g.bind(o, self.t[nd.name])
+
+    def outputs(self):
+        return {self.prog.nodes[o].name: from_cuda(self.t[self.prog.nodes[o].name], self.prog.nodes[o].dtype) for o in self.prog.outputs}
+
+
+def gpu(prog, inputs, executor=None, into=None, reported=False):
+    executor = B.FUSED if executor is None else executor
+    b = Bound(prog, inputs, into)
+    if reported:
+        with pytest.raises(B.AccError) as e:
+            b.g.run(executor)
+        assert e.value.status == "ACC_ERR_INDEX_RANGE"
+    else:
+        b.g.run(executor)
+    return b.outputs()
+
+
+def oracle(prog, inputs, strict=True):
+    arrays = {i: np.asarray(inputs[prog.nodes[i].name]) for i in prog.input_ids()}
+    return interp.run(prog.nodes, arrays, strict=strict)
+
+
+def ints(*v):
+    return np.array(v, np.int64).astype(np.int32)
+
+
+# ---- the definitions, worked by hand ---------------------------------------------------------------------------
+
+def test_block_table_by_hand():
+    prog = W.block_tables(3, 3, 5, 6, 4)
+    got = oracle(prog, {"lens": ints(5, 0, 9), "free": ints(7, 3, 9, 1, 4), "off": ints(0, 2, 2, 5)})
+    table, slots = got.values[3].view(np.int32), got.values[4].view(np.int32)
+    assert table.tolist() == [[7, 3, -1], [-1, -1, -1], [9, 1, 4]]
+    # two new tokens of request 0 at positions 3 and 4, three of request 2 at 6, 7, 8, one of padding
+    assert slots.tolist() == [7 * 4 + 3, 3 * 4 + 0, 1 * 4 + 2, 1 * 4 + 3, 4 * 4 + 0, -1]
+
+
+def test_grown_block_table_by_hand():
+    prog = W.block_tables(3, 3, 2, 3, 4, grow=True)
+    got = oracle(prog, {"lens": ints(5, 4, 2), "free": ints(8, 6), "off": ints(0, 1, 2, 3), "old_lens": ints(4, 3, 9),
+                        "old": np.array([[1, 0, 0], [2, 5, 5], [3, 4, 7]], np.int32)})
+    # request 0 needs a second block, request 1 still fits its first, request 2 was cut down to one block
+    assert got.values[5].view(np.int32).tolist() == [[1, 8, -1], [2, -1, -1], [3, -1, -1]]
+    assert got.values[6].view(np.int32).tolist() == [8 * 4, 2 * 4 + 3, 3 * 4 + 1]
+
+
+def test_put_rows_by_hand():
+    nodes = [Node("input", "f32", (4, 2), name="dest"), Node("input", "i32", (4,), name="slots"), Node("input", "f32", (4, 2), name="rows"),
+             Node("put_rows", "f32", (4, 2), (0, 1, 2), 3, name="out")]
+    got = interp.run(nodes, {0: np.zeros((4, 2), np.float32), 1: ints(2, -1, 0, 2), 2: np.arange(8, dtype=np.float32).reshape(4, 2)})
+    assert got.values[3].tolist() == [[4, 5], [0, 0], [6, 7], [0, 0]]        # of the two rows for slot 2 the last one
+
+
+def test_paged_attention_by_hand():
+    # one head of eight elements, two blocks of two tokens in the order 1, 0; the keys only differ in their first element
+    prog = W.paged_attention(2, 1, 1, 8, 4, 2, 2, "f32", scale=np.log(2.0))
+    keys, values = np.zeros((4, 8), np.float32), np.zeros((4, 8), np.float32)
+    keys[[2, 3, 0, 1], 0] = [0, 1, 2, 5]
+    values[[2, 3, 0, 1], 0] = [7, 14, 21, 1000]
+    q = np.zeros((2, 8), np.float32)
+    q[:, 0] = 1
+    got = oracle(prog, {"q": q, "keys": keys, "values": values, "table": ints(1, 0, 0, 0).reshape(2, 2), "lens": ints(3, 0)})
+    # weights 1, 2, 4 of 7: (7 + 28 + 84) / 7; the second request has no tokens
+    assert got.values[5][0].tolist() == [17.0] + [0.0] * 7 and not got.values[5][1].any()
+    nd = dataclasses.replace(prog.nodes[5], iparam=(2, 8, 2))
+    windowed = O.paged_attention(nd, [q, keys, values, ints(1, 0, 0, 0).reshape(2, 2).view(np.uint32), ints(3, 0).view(np.uint32)])[0]
+    assert abs(windowed[0, 0] - (14 * 2 + 21 * 4) / 6) < 1e-12                # the last two tokens only
+
+
+def test_penalize_by_hand():
+    prog = W.penalized_logits(1, 6, 5, 3, True, "f32")
+    got = oracle(prog, {"logits": np.array([[4, -4, 2, 1, 0, 3]], np.float32), "tokens": ints(0, 1, 1, -1, 2).reshape(1, 5),
+                        "params": np.array([[2, 0.5, 0.25, 1]], np.float32), "bias_ids": ints(3, 0, 3).reshape(1, 3),
+                        "bias": np.array([[1, 10, 2]], np.float32), "mask": np.array([[0b011111]], np.uint32)})
+    # 0: prompt only, halved, + 10; 1: doubled, two later times; 2: halved, once; 3: biased twice; 5: not allowed
+    assert got.values[6].tolist() == [[12.0, -8 - 1 - 0.25, 1 - 0.5 - 0.25, 4.0, 0.0, -np.inf]]
+
+
+def test_oracle_rounds_to_nearest_even():
+    x = np.array([1 + 2.0 ** -9, 1 + 3 * 2.0 ** -8, -1e39, 3.0])
+    assert O.widen(O.narrow(x, "bf16"), "bf16").tolist() == [1.0, 1 + 2.0 ** -6, -np.inf, 3.0]
+    assert O.widen(O.narrow(np.array([1 + 2.0 ** -11, 1 + 3 * 2.0 ** -11]), "f16"), "f16").tolist() == [1.0, 1 + 2.0 ** -9]
+
+
+# ---- what the library accepts and refuses -----------------------------------------------------------------------
+
+def _programs():
+    return [W.block_tables(3, 4, 9, 5, 16), W.block_tables(3, 4, 9, 5, 16, grow=True), W.append_rows(32, 16, 3), W.paged_attention(2, 4, 2, 8, 32, 4, 2),
+            W.penalized_logits(2, 40, 3, 2, True), W.penalized_logits(2, 40, 0, 0, False, "f16")]
+
+
+def test_operators_are_clusters_of_their_own():
+    for prog in _programs():
+        g = B.Graph(prog.nodes, prog.outputs)
+        ops = [i for i, nd in enumerate(prog.nodes) if nd.kind in O.KINDS]
+        F, I = g.edges()
+        oF, oI = L.graph_sets(prog.nodes)
+        assert set(F) == oF == set() and set(I) == oI
+        got = g.enumerate()
+        assert got == L.enumerate_partitions(prog.nodes, prog.outputs)
+        assert all(len({pi[i] for i in ops}) == len(ops) for pi in got) and got
+        pi = g.plan("enumerate", "bytes")
+        assert g.refine_to_kernels()[0] == 0 and all(g.manifest()[i] for i in ops) and pi in got
+
+
+def _small_step():
+    """Combinators before, between and behind operators, few enough nodes to enumerate."""
+    nodes = [
+        Node("input", "i32", (4,), name="old_lens"), Node("input", "i32", (9,), name="free"), Node("input", "f32", (16, 8), name="cache"),
+        Node("input", "f32", (4, 8), name="rows"),
+        Node("map", "i32", (4,), (0,), 1, fn="add_const", iparam=(1,)),
+        Node("block_table", "i32", (4, 2), (4, 1), 2, iparam=(4,)), Node("generate", "i32", (5,), (), 0, fn="iota"),
+        Node("slot_map", "i32", (4,), (5, 4, 6), 3, iparam=(4,)), Node("map", "f32", (16, 8), (2,), 1, fn="affine", fparam=(2.0, 0.0)),
+        Node("put_rows", "f32", (16, 8), (8, 7, 3), 3), Node("map", "f32", (16, 8), (9,), 1, fn="affine", fparam=(1.0, 1.0)),
+        Node("map", "f32", (16, 8), (8,), 1, fn="affine", fparam=(3.0, 0.0)), Node("map", "f32", (16, 8), (9,), 1, fn="affine", fparam=(1.0, 2.0)),
+    ]
+    return nodes, [10, 11, 12]
+
+
+def test_enumeration_with_operators_equals_oracle():
+    nodes, outputs = _small_step()
+    g = B.Graph(nodes, outputs)
+    mine, ref = g.enumerate(), L.enumerate_partitions(nodes, outputs)
+    assert mine == ref and mine
+    for pi in mine:
+        assert pi[11] < pi[9]                                # every other use of the destination comes earlier
+        reads, writes = L.traffic(nodes, outputs, pi)
+        assert g.partition_cost(pi, "reads_writes") == reads + writes
+    # readers of an operator's result share the read as readers of an input do
+    assert any(pi[10] == pi[12] for pi in mine) and any(pi[8] == pi[11] for pi in mine)
+    best = g.plan("branch_bound", "reads_writes")
+    assert g.partition_cost(best, "reads_writes") == min(g.partition_cost(pi, "reads_writes") for pi in mine)
+    assert g.partition_cost(g.plan("greedy_topdown", "bytes"), "bytes") >= g.partition_cost(g.plan("enumerate", "bytes"), "bytes")
+
+
+def test_bytes_of_half_arrays():
+    for dtype, size in (("f32", 4), ("bf16", 2), ("f16", 2)):
+        prog = W.append_rows(32, 16, 3, dtype)
+        g = B.Graph(prog.nodes, prog.outputs)
+        pi = g.plan("enumerate", "bytes")
+        # the destination, the slots and the rows in, the result out, twice
+        assert g.partition_cost(pi, "bytes") == 2 * (32 * 16 * size * 2 + 3 * 4 + 3 * 16 * size)
+        lib = B.lib()
+        need = 32 * 16 * size
+        assert lib.acc_bind(g._h, 0, 256, need) == 0
+        assert B.STATUS_NAME[lib.acc_bind(g._h, 0, 256, need - 1)] == "ACC_ERR_UNBOUND"
+
+
+def _status(nodes, last, **changes):
+    g = B.Graph(nodes)
+    nd = dataclasses.replace(last, **changes)
+    try:
+        g.add_node(nd)
+    except B.AccError as e:
+        return e.status
+    return "ACC_OK"
+
+
+def _with(nodes, i, **changes):
+    return [dataclasses.replace(nd, **changes) if k == i else nd for k, nd in enumerate(nodes)]
+
+
+def _split(prog, node):
+    return prog.nodes[:node], prog.nodes[node]
+
+
+REFUSALS = [
+    # program, the operator's node, an input to change and how (or None), how to change the operator, what it is refused as
+    (W.block_tables(3, 4, 9, 5, 16), 3, None, {"iparam": (0,)}, "ACC_ERR_ARG"),
+    (W.block_tables(3, 4, 9, 5, 16), 3, None, {"iparam": (1 << 31,)}, "ACC_ERR_ARG"),
+    (W.block_tables(3, 4, 9, 5, 16), 3, None, {"inputs": (0, 1, 2), "n_array": 3}, "ACC_ERR_ARG"),
+    (W.block_tables(3, 4, 9, 5, 16), 3, None, {"n_array": 1}, "ACC_ERR_ARG"),
+    (W.block_tables(3, 4, 9, 5, 16), 3, None, {"fn": "add"}, "ACC_ERR_ARG"),
+    (W.block_tables(3, 4, 9, 5, 16), 3, None, {"idx_fn": "reverse"}, "ACC_ERR_ARG"),
+    (W.block_tables(3, 4, 9, 5, 16), 3, None, {"dtype": "f32"}, "ACC_ERR_DTYPE"),
+    (W.block_tables(3, 4, 9, 5, 16), 3, (0, {"dtype": "f32"}), {}, "ACC_ERR_DTYPE"),
+    (W.block_tables(3, 4, 9, 5, 16), 3, None, {"shape": (4, 4)}, "ACC_ERR_SHAPE"),
+    (W.block_tables(3, 4, 9, 5, 16), 3, None, {"shape": (3,)}, "ACC_ERR_SHAPE"),
+    (W.block_tables(3, 4, 9, 5, 16, grow=True), 5, (4, {"shape": (3, 5)}), {}, "ACC_ERR_SHAPE"),
+    (W.block_tables(3, 4, 9, 5, 16), 4, (2, {"shape": (3,)}), {}, "ACC_ERR_SHAPE"),
+    (W.block_tables(3, 4, 9, 5, 16), 4, None, {"shape": (5, 1)}, "ACC_ERR_SHAPE"),
+    (W.block_tables(3, 4, 9, 5, 16), 4, None, {"dtype": "bf16"}, "ACC_ERR_DTYPE"),
+    (W.append_rows(32, 16, 3), 5, (2, {"dtype": "f32"}), {}, "ACC_ERR_DTYPE"),
+    (W.append_rows(32, 16, 3), 5, (3, {"dtype": "f16"}), {}, "ACC_ERR_DTYPE"),
+    (W.append_rows(32, 16, 3), 5, (3, {"shape": (4, 16)}), {}, "ACC_ERR_SHAPE"),
+    (W.append_rows(32, 16, 3), 5, (3, {"shape": (3, 15)}), {}, "ACC_ERR_SHAPE"),
+    (W.append_rows(32, 16, 3), 5, None, {"shape": (31, 16)}, "ACC_ERR_SHAPE"),
+    (W.paged_attention(2, 4, 2, 8, 32, 4, 2), 5, None, {"dtype": "i32"}, "ACC_ERR_DTYPE"),
+    (W.paged_attention(2, 4, 2, 8, 32, 4, 2), 5, (1, {"dtype": "f32"}), {}, "ACC_ERR_DTYPE"),
+    (W.paged_attention(2, 4, 2, 8, 32, 4, 2), 5, (3, {"dtype": "f32"}), {}, "ACC_ERR_DTYPE"),
+    (W.paged_attention(2, 4, 2, 8, 32, 4, 2), 5, None, {"iparam": (4, 4, 0)}, "ACC_ERR_UNSUPPORTED"),
+    (W.paged_attention(2, 4, 2, 8, 32, 4, 2), 5, None, {"iparam": (4, 12, 0)}, "ACC_ERR_UNSUPPORTED"),
+    (W.paged_attention(2, 4, 2, 264, 32, 4, 2), 5, None, {}, "ACC_ERR_UNSUPPORTED"),
+    (W.paged_attention(2, 4, 2, 8, 32, 4, 2), 5, None, {"iparam": (4, 8, -1)}, "ACC_ERR_ARG"),
+    (W.paged_attention(2, 4, 2, 8, 32, 4, 2), 5, None, {"iparam": (0, 8, 0)}, "ACC_ERR_ARG"),
+    (W.paged_attention(2, 4, 3, 8, 32, 4, 2), 5, None, {}, "ACC_ERR_SHAPE"),
+    (W.paged_attention(2, 4, 2, 8, 32, 4, 2), 5, None, {"iparam": (4, 24, 0)}, "ACC_ERR_SHAPE"),
+    (W.paged_attention(2, 4, 2, 8, 32, 4, 2), 5, (2, {"shape": (31, 16)}), {}, "ACC_ERR_SHAPE"),
+    (W.paged_attention(2, 4, 2, 8, 32, 4, 2), 5, (4, {"shape": (3,)}), {}, "ACC_ERR_SHAPE"),
+    (W.paged_attention(2, 4, 2, 8, 32, 4, 2), 5, (1, {"shape": (32, 0)}), {}, "ACC_ERR_SHAPE"),
+    (W.penalized_logits(2, 40, 3, 2, True), 6, None, {"dtype": "f16"}, "ACC_ERR_DTYPE"),
+    (W.penalized_logits(2, 40, 3, 2, True), 6, (1, {"dtype": "f32"}), {}, "ACC_ERR_DTYPE"),
+    (W.penalized_logits(2, 40, 3, 2, True, "f16"), 6, (4, {"dtype": "f16"}), {}, "ACC_ERR_DTYPE"),
+    (W.penalized_logits(2, 40, 3, 2, True), 6, (2, {"shape": (2, 3)}), {}, "ACC_ERR_SHAPE"),
+    (W.penalized_logits(2, 40, 3, 2, True), 6, (3, {"shape": (2, 3)}), {}, "ACC_ERR_SHAPE"),
+    (W.penalized_logits(2, 40, 3, 2, True), 6, (5, {"shape": (2, 1)}), {}, "ACC_ERR_SHAPE"),
+    (W.penalized_logits(2, 40, 3, 2, True), 6, (1, {"shape": (3, 3)}), {}, "ACC_ERR_SHAPE"),
+]
+
+
+@pytest.mark.parametrize("case", range(len(REFUSALS)))
+def test_refusals(case):
+    prog, node, change, op, want = REFUSALS[case]
+    nodes, last = _split(prog, node)
+    if change:
+        nodes = _with(nodes, *change[:1], **change[1])
+    assert _status(nodes, last, **op) == want
+
+
+def test_combinators_refuse_half_arrays():
+    for dtype in ("f16", "bf16"):
+        x = Node("input", dtype, (8,), name="x")
+        assert _status([x], Node("map", "f32", (8,), (0,), 1, fn="identity")) == "ACC_ERR_DTYPE"
+        assert _status([x], Node("map", dtype, (8,), (0,), 1, fn="identity")) == "ACC_ERR_DTYPE"
+        assert _status([x], Node("fold", dtype, (), (0,), 1, fn="add")) == "ACC_ERR_DTYPE"
+        assert _status([], Node("generate", dtype, (8,), (), 0, fn="iota")) == "ACC_ERR_DTYPE"
+        i = Node("input", "i32", (8,), name="i")
+        assert _status([i, x], Node("gather", dtype, (8,), (0, 1), 2)) == "ACC_ERR_DTYPE"
+
+
+def _bind_at(g, prog, addresses):
+    for name, at in addresses.items():
+        i = prog.id(name)
+        assert B.lib().acc_bind(g._h, i, at, 1 << 24) == 0
+
+
+def _schedule_status(prog, addresses, executor=B.FUSED):
+    g = B.Graph(prog.nodes, prog.outputs)
+    g.plan("enumerate", "bytes")
+    _bind_at(g, prog, addresses)
+    try:
+        g.workspace_bytes(executor)
+    except B.AccError as e:
+        return e.status
+    return "ACC_OK"
+
+
+def test_results_do_not_overlap_inputs():
+    far = lambda prog: {nd.name: (i + 1) << 24 for i, nd in enumerate(prog.nodes)}
+    prog = W.append_rows(32, 16, 3)
+    for executor in (B.FUSED, B.UNFUSED):
+        assert _schedule_status(prog, far(prog), executor) == "ACC_OK"
+        assert _schedule_status(prog, far(prog) | {"new_keys": 1 << 24, "new_values": 2 << 24}, executor) == "ACC_OK"       # in place
+        assert _schedule_status(prog, far(prog) | {"new_keys": (1 << 24) + 16}, executor) == "ACC_ERR_ARG"                  # beside itself
+        assert _schedule_status(prog, far(prog) | {"new_keys": 4 << 24}, executor) == "ACC_ERR_ARG"                         # over the rows
+        assert _schedule_status(prog, far(prog) | {"new_keys": (1 << 24) + 32 * 16 * 2}, executor) == "ACC_OK"              # right behind
+    prog = W.paged_attention(2, 4, 2, 8, 32, 4, 2)
+    assert _schedule_status(prog, far(prog) | {"out": 1 << 24}) == "ACC_ERR_ARG"
+    prog = W.penalized_logits(2, 40, 3, 2, True)
+    assert _schedule_status(prog, far(prog) | {"penalized": 1 << 24}) == "ACC_OK"
+    assert _schedule_status(prog, far(prog) | {"penalized": 6 << 24}) == "ACC_ERR_ARG"
+    prog = W.block_tables(3, 4, 9, 5, 16, grow=True)
+    assert _schedule_status(prog, far(prog) | {"table": 5 << 24}) == "ACC_OK"
+    assert _schedule_status(prog, far(prog) | {"table": 4 << 24}) == "ACC_ERR_ARG"
+
+
+def test_what_is_overwritten_is_not_read_later():
+    prog = W.penalized_logits(2, 40, 3, 2, True)
+    for behind in (True, False):
+        nodes = list(prog.nodes)
+        reader = Node("fold", "f32", (2,), (0,), 1, fn="max", name="best")
+        nodes = nodes + [reader] if behind else nodes[:6] + [reader] + nodes[6:]
+        p = W.Program("x", nodes, [6, 7])
+        where = {nd.name: (i + 1) << 24 for i, nd in enumerate(nodes)} | {"penalized": 1 << 24}
+        assert _schedule_status(p, where, B.UNFUSED) == ("ACC_ERR_ILLEGAL_SCATTER" if behind else "ACC_OK")
+
+
+def test_binding_asks_for_the_node_s_element_size():
+    import torch
+    prog = W.append_rows(32, 16, 3)
+    g = B.Graph(prog.nodes, prog.outputs)
+    g.bind_host(0, torch.zeros(32, 16, dtype=torch.bfloat16))
+    with pytest.raises(AssertionError):
+        g.bind_host(0, torch.zeros(32, 16))
+    with pytest.raises(AssertionError):
+        g.bind_host(2, torch.zeros(3, dtype=torch.int16))
+
+
+# ---- kernels against the oracle -----------------------------------------------------------------------------------
+
+def _tables_inputs(rng, R, Wd, block, grow, spare=3, zero=0.2):
+    room = Wd * block
+    lens = rng.integers(0, room + 1, R)
+    lens[rng.random(R) < zero] = 0
+    old = np.minimum(lens, rng.integers(0, room + 1, R)) if grow else np.zeros(R, np.int64)
+    if grow and R > 2:
+        old[R // 2] = room                                   # a request that was cut down
+    need, had = -(-lens // block), -(-old // block)
+    n_free = int(np.maximum(need - had, 0).sum()) + spare
+    counts = np.maximum(lens - old, 0)
+    counts[rng.random(R) < 0.3] = 0
+    off = np.concatenate([[0], np.cumsum(counts)])
+    pool = rng.permutation(n_free + R * Wd + 1)
+    d = {"lens": lens, "free": pool[:n_free], "off": off, "old_lens": old, "old": pool[n_free:n_free + R * Wd].reshape(R, Wd)}
+    return {k: v.astype(np.int32) for k, v in d.items()}, n_free, int(off[-1])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("grow", [False, True])
+@pytest.mark.parametrize("R,Wd,block", [(1, 1, 1), (1, 5000, 3), (3, 0, 16), (7, 3, 16), (256, 9, 7), (257, 8, 16), (1000, 33, 64), (4100, 1, 16), (2100, 2, 1),
+                                        (33, 2049, 1)])
+def test_tables_and_slots(R, Wd, block, grow):
+    rng = np.random.default_rng(R * 7 + Wd)
+    d, n_free, tokens = _tables_inputs(rng, R, Wd, block, grow)
+    prog = W.block_tables(R, Wd, n_free, tokens + 5, block, grow)
+    want = oracle(prog, d)
+    for executor in (B.FUSED, B.UNFUSED):
+        got = gpu(prog, d, executor)
+        for o in prog.outputs:
+            assert np.array_equal(got[prog.nodes[o].name], want.values[o].view(np.uint32)), prog.nodes[o].name
+    if grow:
+        got = gpu(prog, d, into={"table": "old"})
+        assert np.array_equal(got["table"], want.values[prog.id("table")])
+
+
+@pytest.mark.gpu
+def test_slots_of_many_empty_requests():
+    # more than a block's shared memory holds between two tokens of one tile
+    R = 9000
+    counts = np.zeros(R, np.int64)
+    counts[[0, 4000, 8999]] = [3, 1, 2000]
+    off = np.concatenate([[0], np.cumsum(counts)]) + 2                     # (and two tokens that belong to nobody in front)
+    d = {"lens": (counts + 5).astype(np.int32), "off": off.astype(np.int32), "table": (np.arange(R * 300) % 999).reshape(R, 300).astype(np.int32)}
+    nodes = [Node("input", "i32", (R, 300), name="table"), Node("input", "i32", (R,), name="lens"), Node("input", "i32", (R + 1,), name="off"),
+             Node("slot_map", "i32", (2100,), (0, 1, 2), 3, iparam=(8,), name="slots")]
+    prog = W.Program("slots", nodes, [3])
+    assert np.array_equal(gpu(prog, d)["slots"], oracle(prog, d).values[3])
+
+
+@pytest.mark.gpu
+def test_tables_report_numbers_outside_their_range():
+    def both(prog, d):
+        want = oracle(prog, d, strict=False)
+        got = gpu(prog, d, reported=True)
+        for o in prog.outputs:
+            assert np.array_equal(got[prog.nodes[o].name], want.values[o]), prog.nodes[o].name
+    base = {"lens": ints(5, 0, 9), "free": ints(7, 3, 9, 1, 4), "off": ints(0, 2, 2, 5)}
+    both(W.block_tables(3, 2, 5, 6, 4), base)                              # request 2 needs three blocks of two
+    both(W.block_tables(3, 3, 3, 6, 4), base | {"free": ints(7, 3, 9)})    # the list runs out
+    both(W.block_tables(3, 3, 0, 6, 4), base | {"free": ints()})
+    both(W.block_tables(3, 3, 5, 6, 4), base | {"lens": ints(5, -3, 9)})
+    both(W.block_tables(3, 3, 5, 6, 4), base | {"lens": ints(2 ** 31 - 1, 2 ** 31 - 1, 9)})
+    both(W.block_tables(3, 3, 5, 6, 4), base | {"off": ints(0, 6, 6, 9)})  # more new tokens than request 0 has: a position before its first
+
+
+def _put_program(S, C, T, dtype):
+    nodes = [Node("input", dtype, (S, C), name="dest"), Node("input", "i32", (T,), name="slots"), Node("input", dtype, (T, C), name="rows"),
+             Node("put_rows", dtype, (S, C), (0, 1, 2), 3, name="out")]
+    return W.Program("put_rows", nodes, [3])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "i32", "u32", "f16", "bf16"])
+@pytest.mark.parametrize("S,C,T", [(1, 1, 1), (5, 3, 0), (40, 8, 33), (300, 1, 200), (64, 1000, 65), (50, 1027, 40), (3000, 24, 4096), (3000, 24, 4097),
+                                   (700, 5, 9001), (0, 4, 3)])
+def test_put_rows(S, C, T, dtype):
+    rng = np.random.default_rng(S + C + T)
+    bits = lambda *shape: rng.integers(0, 1 << 31, shape).astype(np.uint32 if dtype in ("f32", "i32", "u32") else np.uint16)
+    type_of = {"f32": np.float32, "f16": np.float16}
+    view = lambda a: a.view(type_of.get(dtype, a.dtype))
+    slots = rng.integers(-2, max(S, 1), T).astype(np.int32) if S else np.full(T, -1, np.int32)     # many slots several times
+    d = {"dest": view(bits(S, C)), "slots": slots, "rows": view(bits(T, C))}
+    prog = _put_program(S, C, T, dtype)
+    want = oracle(prog, d).values[3]
+    raw = lambda a: np.ascontiguousarray(a).view(np.uint8)
+    for into in (None, {"out": "dest"}):
+        assert np.array_equal(raw(gpu(prog, d, into=into)["out"]), raw(want))
+
+
+@pytest.mark.gpu
+def test_put_rows_reports_slots_beyond_the_array():
+    d = {"dest": np.zeros((4, 6), np.float32), "slots": ints(3, 4, 0, 2 ** 31 - 1, -2 ** 31), "rows": np.ones((5, 6), np.float32)}
+    prog = _put_program(4, 6, 5, "f32")
+    assert np.array_equal(gpu(prog, d, reported=True)["out"], oracle(prog, d, strict=False).values[3])
+
+
+# An upper bound of |kernel - exact| for the attention, from arithmetic alone.  u = 2^-23 bounds the relative error of a 32-bit
+# operation (twice the half step, for sums that a matrix unit cuts off instead of rounding).
+#   score     a sum of D products: (D + 4) u sum|q k| |scale|; times log2(e) and less the maximum: 3 u |s|
+#   weight    e^error - 1 <= 2 error for errors below 1/2; the exponential itself and every rescaling u each, at most one per token
+#   weights to 16 bits: two parts hold it to 2^-16 (bf16) and 2^-20 (f16)
+#   sums      n + 32 additions for numerator and denominator each
+#   result    half a step of its type, plus half its smallest step
+def attention_bound(nd, inputs, exact, scale_of, dtype):
+    block, D, window = (tuple(nd.iparam) + (0,))[:3]
+    q, k = O.widen(inputs["q"], dtype), O.widen(inputs["keys"], dtype)
+    hq, hk = q.shape[1] // D, k.shape[1] // D
+    u = 2.0 ** -23
+    bound = np.zeros_like(exact)
+    for b in range(q.shape[0]):
+        slots, _ = O.attended_slots(nd, np.asarray(inputs["table"])[b].astype(np.int64), int(inputs["lens"][b]), k.shape[0])
+        n = len(slots)
+        for h in range(hq):
+            if not n:
+                continue
+            qq, kk = np.abs(q[b].reshape(hq, D)[h]), np.abs(k.reshape(-1, hk, D)[slots, h // (hq // hk)])
+            size = abs(nd.fparam[0]) * float((kk @ qq).max())
+            score = (D + 4) * u * size + 3 * u * size
+            split = {"f32": 0.0, "bf16": 2.0 ** -16, "f16": 2.0 ** -20}[dtype]
+            rel = 4 * score + 4 * (n + 32) * u + split
+            cols = slice(h * D, (h + 1) * D)
+            bound[b, cols] = rel * scale_of[b, cols]
+    return bound + np.abs(exact) * EPS[dtype] / 2 * (1 + 2.0 ** -7) + TINY[dtype] + bound * EPS[dtype]
+
+
+def _attention_inputs(rng, B_, hq, hk, D, block, lens, dtype, spare=2, nan=True, width=None):
+    lens = np.asarray(lens, np.int64)
+    need = -(-lens // block)
+    Wd = max(int(need.max()) if need.size else 0, 1) if width is None else width
+    blocks = int(need.sum()) + spare
+    pool = rng.permutation(blocks)
+    table = np.full((B_, Wd), -1, np.int64)
+    keys, values = rng.normal(size=(2, blocks * block, hk * D))
+    live = np.zeros(blocks * block, bool)
+    at = 0
+    for b in range(B_):
+        table[b, :need[b]] = pool[at:at + need[b]]
+        at += need[b]
+        p = np.arange(lens[b])
+        live[table[b, p // block] * block + p % block] = True
+    if nan:                                                  # what nobody attends to may hold anything
+        keys[~live], values[~live] = np.nan, np.inf
+    return {"q": to_type(rng.normal(size=(B_, hq * D)), dtype), "keys": to_type(keys, dtype), "values": to_type(values, dtype),
+            "table": table.astype(np.int32), "lens": lens.astype(np.int32)}
+
+
+def _check_attention(prog, d, got, dtype, strict=True):
+    want = oracle(prog, d, strict=strict)
+    exact, scale_of = want.exact[5], want.abs_sum[5]
+    bound = attention_bound(prog.nodes[5], d, exact, scale_of, dtype)
+    err = np.abs(O.widen(got, dtype) - exact)
+    assert np.all(err <= bound), (float(np.nanmax(err / bound)), np.argwhere(~(err <= bound))[:4].tolist())
+
+
+ATTENTION = [
+    # q heads, kv heads, head size, block, window, lengths
+    (1, 1, 8, 1, 0, [1]),
+    (4, 4, 64, 16, 0, [0, 1, 15, 16, 17, 31, 63, 64, 65, 129, 0]),
+    (8, 1, 128, 16, 0, [700, 3, 0, 64]),
+    (32, 8, 128, 32, 0, [257, 1000]),
+    (16, 2, 128, 128, 100, [99, 100, 101, 640, 5]),
+    (10, 2, 80, 24, 0, [77, 300, 1]),
+    (7, 1, 96, 7, 1, [50, 51]),
+    (18, 1, 40, 5, 0, [333]),
+    (40, 1, 64, 16, 64, [1500, 64]),
+    (6, 3, 256, 64, 0, [100, 513]),
+    (20, 4, 200, 10, 33, [2, 40, 400]),
+    (2, 2, 24, 100, 0, [1000, 0, 0, 0, 0]),
+    (12, 12, 16, 3, 0, list(range(0, 40))),
+]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", REAL)
+@pytest.mark.parametrize("hq,hk,D,block,window,lens", ATTENTION)
+def test_paged_attention(hq, hk, D, block, window, lens, dtype):
+    rng = np.random.default_rng(hq * 1000 + D + len(lens))
+    d = _attention_inputs(rng, len(lens), hq, hk, D, block, lens, dtype)
+    prog = W.paged_attention(len(lens), hq, hk, D, d["keys"].shape[0], block, d["table"].shape[1], dtype, D ** -0.5, window)
+    for executor in (B.FUSED, B.UNFUSED):
+        _check_attention(prog, d, gpu(prog, d, executor)["out"], dtype)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", REAL)
+@pytest.mark.parametrize("lens", [[20000], [9000, 1, 4000, 12000], [30] * 300])
+def test_paged_attention_split_over_blocks(lens, dtype):
+    rng = np.random.default_rng(sum(lens))
+    d = _attention_inputs(rng, len(lens), 4, 2, 64, 16, lens, dtype)
+    prog = W.paged_attention(len(lens), 4, 2, 64, d["keys"].shape[0], 16, d["table"].shape[1], dtype, 0.125)
+    first = gpu(prog, d)["out"]
+    _check_attention(prog, d, first, dtype)
+    assert np.array_equal(first.view(np.uint8), gpu(prog, d)["out"].view(np.uint8))      # the same bits every time
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", REAL)
+def test_paged_attention_of_peaked_and_flat_scores(dtype):
+    """Scores far apart (one token takes all, the running maximum rises late), all alike, and of large magnitude."""
+    rng = np.random.default_rng(3)
+    d = _attention_inputs(rng, 3, 8, 2, 64, 16, [500, 500, 300], dtype)
+    prog = W.paged_attention(3, 8, 2, 64, d["keys"].shape[0], 16, d["table"].shape[1], dtype, 0.125)
+    at = lambda b, p: d["table"][b, p // 16] * 16 + p % 16
+    keys = O.widen(d["keys"], dtype)
+    for p in range(500):
+        keys[at(0, p)] *= 0.02 * p                           # rising
+        keys[at(1, p)] = 0.5                                 # alike
+    keys[at(2, 299)] *= 30                                   # the last one decides
+    d["keys"] = to_type(keys, dtype)
+    _check_attention(prog, d, gpu(prog, d)["out"], dtype)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", REAL)
+def test_paged_attention_reports_numbers_outside_their_range(dtype):
+    rng = np.random.default_rng(11)
+    good = _attention_inputs(rng, 4, 4, 2, 32, 8, [40, 41, 20, 0], dtype, nan=False)
+    S, width = good["keys"].shape[0], good["table"].shape[1]
+    prog = W.paged_attention(4, 4, 2, 32, S, 8, width, dtype, 0.2)
+    for name, change in {"a block beyond the cache": ("table", (0, 2), S // 8), "a huge block": ("table", (0, 2), 2 ** 31 - 1),
+                         "a missing block": ("table", (1, 0), -1), "a negative length": ("lens", (2,), -5),
+                         "a length beyond the table": ("lens", (1,), width * 8 + 1), "a huge length": ("lens", (1,), 2 ** 31 - 1)}.items():
+        d = {k: v.copy() for k, v in good.items()}
+        d[change[0]][change[1]] = change[2]
+        _check_attention(prog, d, gpu(prog, d, reported=True)["out"], dtype, strict=False)
+    # every block of a request missing: nothing to attend to
+    d = {k: v.copy() for k, v in good.items()}
+    d["table"][0] = -1
+    got = gpu(prog, d, reported=True)["out"]
+    assert not O.widen(got, dtype)[0].any()
+
+
+@pytest.mark.gpu
+def test_paged_attention_of_infinities():
+    """As the formula says: a score of -infinity weighs nothing, one of +infinity or not-a-number makes the row not a number."""
+    d = _attention_inputs(np.random.default_rng(5), 3, 1, 1, 16, 8, [30, 30, 30], "f32")
+    prog = W.paged_attention(3, 1, 1, 16, d["keys"].shape[0], 8, d["table"].shape[1], "f32", 1.0)
+    d["q"][:, 0] = 1.0
+    at = lambda b, p: d["table"][b, p // 8] * 8 + p % 8
+    d["keys"][at(0, 3), 0] = -np.inf
+    d["keys"][at(1, 4), 0] = np.inf
+    d["keys"][at(2, 5), 0] = np.nan
+    got = gpu(prog, d)["out"]
+    want = oracle(prog, d).exact[5]
+    assert np.isnan(want[1:]).all() and np.isnan(got[1:]).all()
+    assert np.all(np.abs(got[0] - want[0]) <= 1e-5) and np.isfinite(got[0]).all()
+
+
+@pytest.mark.gpu
+def test_paged_attention_over_a_cache_beyond_32_bit_offsets():
+    """Slots at the end of a cache of nearly 2^31 elements (4 GiB): byte offsets that 32 bits do not hold."""
+    import torch
+    hk, D, block = 8, 128, 64
+    S = (2 ** 31 - 2 ** 16) // (hk * D) // block * block
+    blocks = S // block
+    d = _attention_inputs(np.random.default_rng(9), 2, 8, hk, D, block, [100, 70], "bf16", spare=0, nan=False)
+    prog = W.paged_attention(2, 8, hk, D, S, block, d["table"].shape[1], "bf16", D ** -0.5)
+    used = int(d["table"].max()) + 1
+    far = torch.empty(2, S, hk * D, dtype=torch.bfloat16, device="cuda")
+    g = B.Graph(prog.nodes, prog.outputs)
+    g.plan("enumerate", "bytes")
+    for k, name in enumerate(("keys", "values")):
+        far[k, S - used * block:] = to_cuda(d[name], "bf16")
+        g.bind(prog.id(name), far[k])
+    table = np.where(d["table"] >= 0, d["table"] + blocks - used, -1).astype(np.int32)
+    g.bind(prog.id("q"), to_cuda(d["q"], "bf16"))
+    g.bind(prog.id("table"), to_cuda(table, "i32"))
+    g.bind(prog.id("lens"), to_cuda(d["lens"], "i32"))
+    out = torch.empty(2, 8 * D, dtype=torch.bfloat16, device="cuda")
+    g.bind(prog.id("out"), out)
+    g.run(B.FUSED)
+    _check_attention(W.paged_attention(2, 8, hk, D, used * block, block, d["table"].shape[1], "bf16", D ** -0.5), d, from_cuda(out, "bf16"), "bf16")
+    # rows put at the far end
+    put = _put_program(S, hk * D, 3, "bf16")
+    p = B.Graph(put.nodes, put.outputs)
+    p.plan("enumerate", "bytes")
+    rows = torch.randn(3, hk * D, device="cuda").to(torch.bfloat16)
+    p.bind(0, far[0])
+    p.bind(1, torch.tensor([S - 1, 0, S - 2], dtype=torch.int32, device="cuda"))
+    p.bind(2, rows)
+    p.bind(3, far[0])
+    before = far[0, S - 3].clone()
+    p.run(B.FUSED)
+    assert torch.equal(far[0, [S - 1, 0, S - 2]], rows) and torch.equal(far[0, S - 3], before)
+
+
+def _penalty_inputs(rng, B_, V, Lh, K, masked, dtype):
+    logits = to_type(4 * rng.normal(size=(B_, V)), dtype)
+    tokens = (V * rng.random((B_, Lh)) ** 3).astype(np.int64).clip(0, V - 1)
+    tokens[rng.random((B_, Lh)) < 0.3] = -1
+    ids = rng.integers(-1, V, (B_, K))
+    params = np.stack([1 + rng.random(B_), rng.random(B_), rng.random(B_), rng.integers(0, Lh + 1, B_)], 1).astype(np.float32)
+    words = -(-V // 32) if masked else 0
+    return {"logits": logits, "tokens": tokens.astype(np.int32), "params": params, "bias_ids": ids.astype(np.int32),
+            "bias": (10 * rng.random((B_, K)) - 5).astype(np.float32), "mask": rng.integers(0, 1 << 32, (B_, words)).astype(np.uint32)}
+
+
+def _check_penalties(prog, d, got, dtype, strict=True):
+    """Every operation rounds once: a quotient or product, a product and two differences for the counts, as many additions as
+    a column has biases, all of magnitudes below mag."""
+    want = oracle(prog, d, strict=strict)
+    exact, mag = want.exact[6], want.abs_sum[6]
+    got = O.widen(got, dtype)
+    same = np.isinf(exact) | np.isnan(exact)
+    assert np.array_equal(got[same], exact[same], equal_nan=True)
+    K = d["bias_ids"].shape[1]
+    bound = (8 + K) * 2.0 ** -24 * mag + np.abs(exact) * EPS[dtype] / 2 * (1 + 2.0 ** -7) + TINY[dtype]
+    # (the oracle rounds to the type once more than needed: its own exact value is compared)
+    err = np.abs(got[~same] - exact[~same])
+    assert np.all(err <= bound[~same] * (1 + EPS[dtype])), float((err / bound[~same]).max())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", REAL)
+@pytest.mark.parametrize("B_,V,Lh,K,masked", [(1, 1, 3, 1, True), (3, 7, 20, 9, True), (2, 33, 0, 0, True), (5, 32, 1, 0, False), (2, 4096, 500, 0, True),
+                                              (2, 4097, 300, 40, True), (3, 8191, 0, 70, False), (2, 8197, 1000, 3, True), (1, 50001, 9000, 300, True),
+                                              (2, 24576, 0, 0, False), (4, 0, 3, 2, False)])
+def test_penalties(B_, V, Lh, K, masked, dtype):
+    if V == 0:
+        d = {"logits": to_type(np.zeros((B_, 0)), dtype), "tokens": np.full((B_, Lh), -1, np.int32), "params": np.ones((B_, 4), np.float32),
+             "bias_ids": np.full((B_, K), -1, np.int32), "bias": np.zeros((B_, K), np.float32), "mask": np.zeros((B_, 0), np.uint32)}
+    else:
+        d = _penalty_inputs(np.random.default_rng(V + Lh), B_, V, Lh, K, masked, dtype)
+    prog = W.penalized_logits(B_, V, Lh, K, masked, dtype)
+    for into in (None, {"penalized": "logits"}):
+        _check_penalties(prog, d, gpu(prog, d, into=into)["penalized"], dtype)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", REAL)
+def test_penalties_of_infinities_and_repeated_biases(dtype):
+    d = _penalty_inputs(np.random.default_rng(2), 3, 1001, 50, 200, True, dtype)
+    logits = O.widen(d["logits"], dtype)
+    logits[0, ::5], logits[1, ::7], logits[2, ::3] = -np.inf, np.inf, np.nan
+    d["logits"] = to_type(logits, dtype)
+    d["bias_ids"][:, ::3] = 17                               # many biases of one column
+    d["bias_ids"][1, :] = 1000
+    prog = W.penalized_logits(3, 1001, 50, 200, True, dtype)
+    first = gpu(prog, d)["penalized"]
+    _check_penalties(prog, d, first, dtype)
+    assert np.array_equal(first.view(np.uint8), gpu(prog, d)["penalized"].view(np.uint8))
+
+
+@pytest.mark.gpu
+def test_penalties_report_numbers_outside_their_range():
+    d = _penalty_inputs(np.random.default_rng(4), 2, 500, 30, 4, False, "f32")
+    prog = W.penalized_logits(2, 500, 30, 4, False)
+    for name in ("tokens", "bias_ids"):
+        bad = {k: v.copy() for k, v in d.items()}
+        bad[name][1, 2] = 500
+        bad[name][1, 3] = 2 ** 31 - 1
+        _check_penalties(prog, bad, gpu(prog, bad, reported=True)["penalized"], "f32", strict=False)
+
+
+@pytest.mark.gpu
+def test_more_rows_than_a_grid_has():
+    B_ = 70000
+    d = _penalty_inputs(np.random.default_rng(6), B_, 5, 2, 1, True, "f32")
+    prog = W.penalized_logits(B_, 5, 2, 1, True)
+    _check_penalties(prog, d, gpu(prog, d)["penalized"], "f32")
+
+
+# ---- a run of them together ----------------------------------------------------------------------------------------
+
+def _step_inputs(rng, R=5, hq=4, hk=2, D=16, block=4, V=100, dtype="f32"):
+    lens = rng.integers(1, 30, R)
+    had = -(-lens // block)
+    width = 10
+    blocks = int(had.sum()) + R + 2
+    pool = rng.permutation(blocks)
+    old = np.full((R, width), -1, np.int64)
+    at = 0
+    for r in range(R):
+        old[r, :had[r]] = pool[at:at + had[r]]
+        at += had[r]
+    S, c = blocks * block, hk * D
+    normal = lambda *s: to_type(rng.normal(size=s), dtype)
+    d = {"old_lens": lens.astype(np.int32), "free": pool[at:].astype(np.int32), "old": old.astype(np.int32), "q": normal(R, hq * D), "k": normal(R, c),
+         "v": normal(R, c), "keys": normal(S, c), "values": normal(S, c), "logits": to_type(rng.normal(size=(R, V)), "f32"),
+         "tokens": rng.integers(-1, V, (R, 12)).astype(np.int32), "params": np.tile(np.array([[1.25, 0.5, 0.25, 3]], np.float32), (R, 1)),
+         "bias_ids": np.zeros((R, 0), np.int32), "bias": np.zeros((R, 0), np.float32), "mask": np.zeros((R, 0), np.uint32)}
+    return W.decode_step(R, hq, hk, D, S, block, width, blocks - at, V, 12, dtype), d
+
+
+def _check_step(prog, d, got, dtype):
+    want = oracle(prog, d)
+    for name in ("table", "new_keys", "new_values"):
+        i = prog.id(name)
+        assert np.array_equal(np.ascontiguousarray(got[name]).view(np.uint8), np.ascontiguousarray(want.values[i]).view(np.uint8)), name
+    i = prog.id("out")
+    nd = prog.nodes[i]
+    seen = {"q": d["q"], "keys": want.values[prog.id("new_keys")], "values": want.values[prog.id("new_values")],
+            "table": want.values[prog.id("table")].view(np.int32), "lens": d["old_lens"] + 1}
+    bound = attention_bound(nd, seen, want.exact[i], want.abs_sum[i], dtype)
+    assert np.all(np.abs(O.widen(got["out"], dtype) - want.exact[i]) <= bound)
+    i = prog.id("penalized")
+    err = np.abs(got["penalized"].astype(np.float64) - want.exact[i])
+    assert np.all(err <= 9 * 2.0 ** -24 * want.abs_sum[i] + np.abs(want.exact[i]) * 2.0 ** -23)
+    assert np.array_equal(got["best"], got["penalized"].max(1))
+
+
+IN_PLACE = {"new_keys": "keys", "new_values": "values", "table": "old", "penalized": "logits"}
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", REAL)
+def test_a_decode_step(dtype):
+    prog, d = _step_inputs(np.random.default_rng(1), dtype=dtype)
+    for executor in (B.FUSED, B.UNFUSED):
+        _check_step(prog, d, gpu(prog, d, executor), dtype)
+        _check_step(prog, d, gpu(prog, d, executor, into=IN_PLACE), dtype)
+
+
+@pytest.mark.gpu
+def test_decode_steps_on_another_stream_and_replayed():
+    """The same handle run on a side stream, then captured into a CUDA graph and replayed over data that changed meanwhile."""
+    import torch
+    prog, d = _step_inputs(np.random.default_rng(2), dtype="bf16")
+    _, other = _step_inputs(np.random.default_rng(2), dtype="bf16")
+    other["q"], other["old_lens"] = to_type(np.random.default_rng(8).normal(size=d["q"].shape), "bf16"), d["old_lens"] - 1
+    b = Bound(prog, d)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        b.g.run(B.FUSED)
+    _check_step(prog, d, b.outputs(), "bf16")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        b.g.run(B.FUSED, finish=False)
+    for data in (other, d):
+        for name in ("q", "old_lens"):
+            nd = prog.nodes[prog.id(name)]
+            b.t[name].copy_(to_cuda(data[name], nd.dtype))
+        graph.replay()
+        torch.cuda.synchronize()
+        b.g.finish()
+        _check_step(prog, data, b.outputs(), "bf16")
+
+
+@pytest.mark.gpu
+def test_operators_end_to_end_from_host_buffers():
+    import torch
+    prog, d = _step_inputs(np.random.default_rng(4), dtype="f16")
+    b = Bound(prog, d)
+    host = {}
+    for i in prog.input_ids():
+        nd = prog.nodes[i]
+        host[nd.name] = b.t[nd.name].cpu()
+        b.t[nd.name].zero_()
+        b.g.bind_host(i, host[nd.name])
+    back = torch.zeros(prog.nodes[prog.id("out")].shape, dtype=torch.float16)
+    b.g.bind_host(prog.id("out"), back)
+    up, down = b.g.run_e2e(B.FUSED)
+    assert up == sum(t.numel() * t.element_size() for t in host.values()) and down == back.numel() * 2
+    _check_step(prog, d, b.outputs(), "f16")
+    assert torch.equal(back, b.t["out"].cpu())

@@ -14,6 +14,14 @@ inputs, so every list is a DAG in topological order.  Slot layout by kind:
   scanl/scanr  [src]                           inclusive, per innermost row (exclusive=True: seeded, exclusive)
   foldseg      [src, offsets]                  n_array = 1; ys[s] = fold of src[offsets[s] .. offsets[s+1])
 
+Operators (foreign functions; every slot is an array slot):
+
+  block_table      [lens, free] or [lens, free, old_lens, old]     iparam = (block,)
+  slot_map         [table, lens, off]                               iparam = (block,)
+  put_rows         [dest, slots, rows]
+  paged_attention  [q, keys, values, table, lens]                   iparam = (block, head_dim, window), fparam = (scale,)
+  penalize         [logits, tokens, params, bias_ids, bias, mask]
+
 Slots at positions >= n_array are "free variable" reads (element-level
 indexing: element 0, except the offsets of a foldseg, which are read at s and s+1).  Function names are interpreted by each
 executor's own table; this file only spells them.
@@ -25,7 +33,7 @@ from typing import List, Tuple
 @dataclass
 class Node:
     kind: str
-    dtype: str                      # 'f32' | 'i32' | 'u32'
+    dtype: str                      # 'f32' | 'i32' | 'u32'; what only operators read and write: also 'f16' | 'bf16'
     shape: Tuple[int, ...]          # () for the scalar result of a rank-1 fold
     inputs: Tuple[int, ...] = ()
     n_array: int = 0
@@ -673,3 +681,70 @@ def random_int_program(seed, n=4099, rows=None):
     outputs = [i for i, nd in enumerate(nodes) if nd.kind != "input" and i not in used]
     return Program("random_int%s_%d" % ("" if rows is None else "sq" if rows == n else "2d", seed), nodes, outputs,
                    index_bound={"idx": count})
+
+
+# --------------------------------------------------------------------------
+# A decode step of a language model: operators, and combinators around them
+# --------------------------------------------------------------------------
+
+def _op(kind, dtype, shape, inputs, name, iparam=(), fparam=()):
+    return Node(kind, dtype, tuple(shape), tuple(inputs), len(inputs), iparam=tuple(iparam), fparam=tuple(fparam), name=name)
+
+
+def block_tables(requests, width, n_free, tokens, block, grow=False):
+    """Block tables of `requests` requests and the slots of the batch's `tokens` new tokens; grow: from the tables of the step before."""
+    nodes = [_inp("lens", "i32", (requests,)), _inp("free", "i32", (n_free,)), _inp("off", "i32", (requests + 1,))]
+    if grow:
+        nodes += [_inp("old_lens", "i32", (requests,)), _inp("old", "i32", (requests, width))]
+    t = len(nodes)
+    nodes.append(_op("block_table", "i32", (requests, width), (0, 1, 3, 4) if grow else (0, 1), "table", (block,)))
+    nodes.append(_op("slot_map", "i32", (tokens,), (t, 0, 2), "slots_of_tokens", (block,)))
+    return Program("block_tables", nodes, [t, t + 1])
+
+
+def append_rows(slots, cols, tokens, dtype="bf16"):
+    """New keys and values put into a cache of `slots` rows (bind the results to the caches' own buffers)."""
+    nodes = [_inp("keys", dtype, (slots, cols)), _inp("values", dtype, (slots, cols)), _inp("slots", "i32", (tokens,)),
+             _inp("k", dtype, (tokens, cols)), _inp("v", dtype, (tokens, cols)),
+             _op("put_rows", dtype, (slots, cols), (0, 2, 3), "new_keys"), _op("put_rows", dtype, (slots, cols), (1, 2, 4), "new_values")]
+    return Program("append_rows", nodes, [5, 6])
+
+
+def paged_attention(batch, q_heads, kv_heads, head_dim, slots, block, width, dtype="bf16", scale=1.0, window=0):
+    """One new token per request over its paged keys and values."""
+    nodes = [_inp("q", dtype, (batch, q_heads * head_dim)), _inp("keys", dtype, (slots, kv_heads * head_dim)),
+             _inp("values", dtype, (slots, kv_heads * head_dim)), _inp("table", "i32", (batch, width)), _inp("lens", "i32", (batch,)),
+             _op("paged_attention", dtype, (batch, q_heads * head_dim), (0, 1, 2, 3, 4), "out", (block, head_dim, window), (scale,))]
+    return Program("paged_attention", nodes, [5])
+
+
+def penalized_logits(batch, vocabulary, history, biases, masked, dtype="f32"):
+    """Penalties for tokens seen before, biases and a mask on rows of logits."""
+    words = -(-vocabulary // 32) if masked else 0
+    nodes = [_inp("logits", dtype, (batch, vocabulary)), _inp("tokens", "i32", (batch, history)), _inp("params", "f32", (batch, 4)),
+             _inp("bias_ids", "i32", (batch, biases)), _inp("bias", "f32", (batch, biases)), _inp("mask", "u32", (batch, words)),
+             _op("penalize", dtype, (batch, vocabulary), range(6), "penalized")]
+    return Program("penalized_logits", nodes, [6])
+
+
+def decode_step(requests, q_heads, kv_heads, head_dim, slots, block, width, n_free, vocabulary, history, dtype="f32"):
+    """One step of every request: lengths grow by one (a map), tables and slots follow, the new keys and values go into the
+    cache, the queries attend, penalties fall on logits, and a fold takes each row's largest."""
+    c, R = kv_heads * head_dim, requests
+    nodes = [
+        _inp("old_lens", "i32", (R,)), _inp("free", "i32", (n_free,)), _inp("old", "i32", (R, width)),
+        _inp("q", dtype, (R, q_heads * head_dim)), _inp("k", dtype, (R, c)), _inp("v", dtype, (R, c)),
+        _inp("keys", dtype, (slots, c)), _inp("values", dtype, (slots, c)),
+        _inp("logits", "f32", (R, vocabulary)), _inp("tokens", "i32", (R, history)), _inp("params", "f32", (R, 4)),
+        _inp("bias_ids", "i32", (R, 0)), _inp("bias", "f32", (R, 0)), _inp("mask", "u32", (R, 0)),
+        Node("map", "i32", (R,), (0,), 1, fn="add_const", iparam=(1,), name="lens"),
+        Node("generate", "i32", (R + 1,), (), 0, fn="iota", name="off"),
+        _op("block_table", "i32", (R, width), (14, 1, 0, 2), "table", (block,)),
+        _op("slot_map", "i32", (R,), (16, 14, 15), "new_slots", (block,)),
+        _op("put_rows", dtype, (slots, c), (6, 17, 4), "new_keys"),
+        _op("put_rows", dtype, (slots, c), (7, 17, 5), "new_values"),
+        _op("paged_attention", dtype, (R, q_heads * head_dim), (3, 18, 19, 16, 14), "out", (block, head_dim, 0), (head_dim ** -0.5,)),
+        _op("penalize", "f32", (R, vocabulary), (8, 9, 10, 11, 12, 13), "penalized"),
+        Node("fold", "f32", (R,), (21,), 1, fn="max", name="best"),
+    ]
+    return Program("decode_step", nodes, [16, 18, 19, 20, 21, 22])

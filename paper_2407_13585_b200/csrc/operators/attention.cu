@@ -1,4 +1,22 @@
 // Attention of one new token per request over its paged keys and values (ACC_PAGED_ATTENTION).
+//
+//   out[b, h] = sum_t w_t v_t / sum_t w_t,   w_t = 2^(s_t - m),   s_t = log2(e) scale q[b, h].k_t,   m = max_t s_t
+//
+// in one pass over keys and values: with a running maximum m, sums and products so far are multiplied by 2^(m - m') when a
+// larger m' turns up, and two runs over different tokens join the same way.  Keys and values are read once (that is what
+// bounds it: 2 e D bytes per token and key head for 4 D (Hq / Hk) operations), so the query heads of a key head are
+// worked on together, eight or sixteen at a time.
+//
+// Splitting.  The work is the list of all tiles (four warps x 16 or 8 tokens) of all requests and key heads, one unit
+// (request, block of heads) after the other; every block of a grid that fills the GPU once takes an equal run of that
+// list, whatever the lengths are.  It finds its place by adding up the lengths itself.  A unit that ends inside one block
+// is finished there; of one that does not, every block leaves its sums in scratch and k_join adds them up in the order of
+// the blocks: no atomics, the same bits every time.
+//
+// Inside a block every warp takes its 16 (8) tokens of a tile through a ring of stages of its own in shared memory, filled
+// by 16-byte asynchronous copies two tiles ahead, across units; the block numbers are read one tile further ahead.
+#include <cfloat>
+
 #include "operators/common.cuh"
 
 namespace acc {
@@ -11,84 +29,807 @@ struct AttentionArgs {
   const int *table, *lens;
   void* out;
   int B, W, S, Hq, Hk, D, window;
-  float scale;
+  int group, units;       // query heads of a key head, units of a request
+  float scale_log2;       // log2(e) scale
   Divisor block;
+  float* parts;           // two records of sums per block of the grid; null: no unit is split
+  int4* joins;            // per block of the grid: {request, unit, last block of it, 0} of the split unit that starts there
 };
 
-// out = sum_t exp(s_t - m) v_t / sum_t exp(s_t - m), s_t = scale q.k_t, with the running maximum m.  A block per request and
-// head; its four warps take every fourth token, lanes share the dimensions, and the warps' sums are joined at the end.
-template <class T>
-__global__ void __launch_bounds__(128) k_attention_simple(AttentionArgs a) {
-  const int b = blockIdx.x, h = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int g = h / (a.Hq / a.Hk);
-  float q[8], acc[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int d = lane + 32 * i;
-    q[i] = d < a.D ? widen<T>(static_cast<const T*>(a.q)[((size_t)b * a.Hq + h) * a.D + d]) : 0.0f;
-    acc[i] = 0;
-  }
+constexpr int kWarps = 4, kThreads = kWarps * 32;
+
+// The tokens [first, end) that request b attends to.
+struct Span {
+  int first, end;
+};
+__device__ __forceinline__ Span span_of(const AttentionArgs& a, int b) {
   const int length = a.lens[b];
-  const long long room = (long long)a.W * a.block.d;
-  const int n = (int)min((long long)max(length, 0), room);
-  bool bad = length < 0 || length > room;
-  float m = -INFINITY, l = 0;
-  bool any = false;                                        // (no score but -infinity is not the same as no token)
-  for (int t = (a.window > 0 ? max(n - a.window, 0) : 0) + warp; t < n; t += 4) {
-    const int p = (int)((uint32_t)t / a.block);
-    const int page = a.table[(size_t)b * a.W + p];
-    const long long at = (long long)page * a.block.d + (t - p * (int)a.block.d);
-    if (page < 0 || at >= a.S) {
-      bad = true;
-      continue;
+  const int end = (int)min((long long)max(length, 0), (long long)a.W * a.block.d);
+  return {a.window > 0 ? max(end - a.window, 0) : 0, end};
+}
+template <int TILE>
+__device__ __forceinline__ int tiles_of(Span s) { return (int)(((uint32_t)(s.end - s.first) + TILE - 1) / TILE); }
+
+// A place in the list of tiles.
+template <int TILE>
+struct Cursor {
+  int b, unit, tile, tiles;
+  Span span;
+  long long left;          // tiles of this block's run, this one included
+
+  __device__ __forceinline__ void enter(const AttentionArgs& a) {
+    span = span_of(a, b);
+    tiles = tiles_of<TILE>(span);
+  }
+  __device__ __forceinline__ void advance(const AttentionArgs& a) {
+    if (--left <= 0) return;
+    if (++tile < tiles) return;
+    tile = 0;
+    if (++unit < a.units) return;
+    unit = 0;
+    do {                                       // (left > 0: there is a request with tokens behind)
+      ++b;
+      enter(a);
+    } while (tiles == 0 && b + 1 < a.B);
+  }
+};
+
+struct Place {
+  long long total;           // tiles of all requests
+  int blocks;                // blocks that have any: each has at least one
+  int b;                     // the request that the run starts in
+  long long b_start;         // tiles before that request
+};
+__device__ __forceinline__ long long run_start(int block, long long total, int blocks) { return (long long)block * total / blocks; }
+
+// Where this block's run of the list starts.  Every thread adds up a share of the requests; requests without tokens get
+// their zeros here, spread over the grid.
+template <class T, int TILE>
+__device__ Cursor<TILE> find_place(const AttentionArgs& a, Place* shared, long long* sums) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int share = (a.B + kThreads - 1) / kThreads;
+  const int r0 = min((int)threadIdx.x * share, a.B), r1 = min(r0 + share, a.B);
+  long long mine = 0;
+  bool bad = false;
+  for (int r = r0; r < r1; ++r) {
+    const int length = a.lens[r];
+    bad = bad || length < 0 || length > (long long)a.W * a.block.d;
+    mine += tiles_of<TILE>(span_of(a, r));
+  }
+  if (bad) raise_index(a.report);
+  mine *= a.units;
+  long long upto = mine;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const long long below = __shfl_up_sync(~0u, upto, d);
+    if (lane >= d) upto += below;
+  }
+  if (lane == 31) sums[warp] = upto;
+  __syncthreads();
+  long long total = 0;
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) {
+    if (w < warp) upto += sums[w];
+    total += sums[w];
+  }
+  const int blocks = (int)min((long long)gridDim.x, total);
+  const bool any = (int)blockIdx.x < blocks;
+  const long long start = any ? run_start(blockIdx.x, total, blocks) : 0, end = any ? run_start(blockIdx.x + 1, total, blocks) : 0;
+  if (any && upto - mine <= start && start < upto) {
+    long long at = upto - mine;
+    int r = r0;
+    for (;; ++r) {
+      const long long n = (long long)tiles_of<TILE>(span_of(a, r)) * a.units;
+      if (at + n > start) break;
+      at += n;
     }
-    any = true;
-    const size_t base = ((size_t)at * a.Hk + g) * a.D;
-    float s = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (lane + 32 * i < a.D) s = fmaf(q[i], widen<T>(static_cast<const T*>(a.keys)[base + lane + 32 * i]), s);
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(~0u, s, d);
-    s *= a.scale;
-    const float top = fmaxf(m, s);
-    const float fall = top == -INFINITY ? 1.0f : expf(m - top), p_t = top == -INFINITY ? 0.0f : expf(s - top);
-    l = l * fall + p_t;
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (lane + 32 * i < a.D) acc[i] = fmaf(p_t, widen<T>(static_cast<const T*>(a.values)[base + lane + 32 * i]), acc[i] * fall);
-    m = top;
+    *shared = {total, blocks, r, at};
   }
-  if (bad && lane == 0) raise_index(a.report);
-  __shared__ float ms[4], ls[4], sums[4][256];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) sums[warp][lane + 32 * i] = acc[i];
-  if (lane == 0) ms[warp] = m, ls[warp] = l;
-  any = __syncthreads_or(any);
-  const float top = fmaxf(fmaxf(ms[0], ms[1]), fmaxf(ms[2], ms[3]));
-  float all = 0;
-  for (int w = 0; w < 4; ++w) all += top == -INFINITY ? 0.0f : ls[w] * expf(ms[w] - top);
-  for (int d = threadIdx.x; d < a.D; d += 128) {
-    float x = 0;
-    for (int w = 0; w < 4; ++w) x += top == -INFINITY ? 0.0f : sums[w][d] * expf(ms[w] - top);
-    static_cast<T*>(a.out)[((size_t)b * a.Hq + h) * a.D + d] = narrow<T>(any ? x / all : 0.0f);
+  for (int r = blockIdx.x; r < a.B; r += gridDim.x) {
+    const Span s = span_of(a, r);
+    if (s.first < s.end) continue;
+    for (int d = threadIdx.x; d < a.Hq * a.D; d += kThreads) static_cast<T*>(a.out)[(size_t)r * a.Hq * a.D + d] = narrow<T>(0.0f);
   }
+  __syncthreads();
+  Cursor<TILE> c{};
+  if (!any) return c;
+  c.b = shared->b;
+  c.enter(a);
+  const long long inside = start - shared->b_start;
+  c.unit = (int)(inside / c.tiles);
+  c.tile = (int)(inside - (long long)c.unit * c.tiles);
+  c.left = end - start;
+  return c;
+}
+
+// The four warps' sums of a unit's tiles [from, ...) that this block had, in shared memory: sums[warp][row][pitch], their
+// maxima and weights in ml[0][warp][row], ml[1][warp][row].  Written out if they are the whole unit, else to scratch.
+// The weights of a row without any token have the maximum -infinity; with tokens it is at least -FLT_MAX.
+template <class T, int DP, int ROWS, int PITCH, int TILE>
+__device__ __forceinline__ void finish_unit(const AttentionArgs& a, const Cursor<TILE>& c, bool from_start, bool to_end,
+                                            const float* sums, const float* ml) {
+  const int head0 = c.unit % (a.units / a.Hk) * ROWS, kv = c.unit / (a.units / a.Hk);
+  const int rows = min(ROWS, a.group - head0);
+  const bool whole = from_start && to_end;
+  float* part = a.parts + (size_t)(blockIdx.x * 2 + (from_start ? 1 : 0)) * ROWS * (DP + 2);
+  for (int i = threadIdx.x; i < rows * (DP / 4); i += kThreads) {
+    const int row = i / (DP / 4), d = i % (DP / 4) * 4;
+    float top = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) top = fmaxf(top, ml[w * ROWS + row]);
+    const float ref = top == -INFINITY ? 0.0f : top;
+    float l = 0, x[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+      const float weight = exp2f(ml[w * ROWS + row] - ref);
+      const float4 s = *reinterpret_cast<const float4*>(sums + (size_t)(w * ROWS + row) * PITCH + d);
+      l = fmaf(ml[(kWarps + w) * ROWS + row], weight, l);
+      x[0] = fmaf(s.x, weight, x[0]), x[1] = fmaf(s.y, weight, x[1]), x[2] = fmaf(s.z, weight, x[2]), x[3] = fmaf(s.w, weight, x[3]);
+    }
+    if (whole) {
+      if (d >= a.D) continue;
+      T* out = static_cast<T*>(a.out) + ((size_t)c.b * a.Hq + (size_t)kv * a.group + head0 + row) * a.D + d;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) out[k] = narrow<T>(top == -INFINITY ? 0.0f : __fdiv_rn(x[k], l));
+    } else {
+      *reinterpret_cast<float4*>(part + row * DP + d) = make_float4(x[0], x[1], x[2], x[3]);
+      if (d == 0) {
+        part[ROWS * DP + row] = top;
+        part[ROWS * DP + ROWS + row] = l;
+      }
+    }
+  }
+}
+
+// Sums of a split unit, one row of heads to a block: maxima first, then the records, four dimensions to a lane.
+template <class T, int DP, int ROWS>
+__global__ void __launch_bounds__(256) k_join(AttentionArgs a) {
+  constexpr int LANES = DP / 4 < 32 ? DP / 4 : 32;         // lanes that share a record's row
+  constexpr int VECS = DP / 4 / LANES, AT_ONCE = 256 / LANES;
+  __shared__ float tops[8], share[AT_ONCE];
+  __shared__ float4 sums[AT_ONCE][LANES * VECS];
+  cudaGridDependencySynchronize();
+  const int4 join = a.joins[blockIdx.x];
+  if (join.x < 0) return;
+  const int per = a.units / a.Hk, head0 = join.y % per * ROWS, row = blockIdx.y;
+  if (row >= a.group - head0) return;
+  const int n = join.z - (int)blockIdx.x + 1;
+  constexpr size_t RECORD = (size_t)ROWS * (DP + 2);
+  const auto record = [&](int i) { return a.parts + ((size_t)(blockIdx.x + i) * 2 + (i == 0 ? 1 : 0)) * RECORD; };
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  float top = -INFINITY;
+  for (int i = threadIdx.x; i < n; i += 256) top = fmaxf(top, record(i)[ROWS * DP + row]);
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
+  if (lane == 0) tops[warp] = top;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < 8; ++w) top = fmaxf(top, tops[w]);
+  const float ref = top == -INFINITY ? 0.0f : top;
+  const int who = threadIdx.x / LANES, at = threadIdx.x % LANES;
+  float l = 0;
+  float4 x[VECS];
+#pragma unroll
+  for (int v = 0; v < VECS; ++v) x[v] = make_float4(0, 0, 0, 0);
+#pragma unroll 4
+  for (int i = who; i < n; i += AT_ONCE) {
+    const float* r = record(i);
+    const float weight = exp2f(r[ROWS * DP + row] - ref);
+    l = fmaf(r[ROWS * DP + ROWS + row], weight, l);
+#pragma unroll
+    for (int v = 0; v < VECS; ++v) {
+      const float4 s = *reinterpret_cast<const float4*>(r + row * DP + (at + v * LANES) * 4);
+      x[v].x = fmaf(s.x, weight, x[v].x), x[v].y = fmaf(s.y, weight, x[v].y), x[v].z = fmaf(s.z, weight, x[v].z), x[v].w = fmaf(s.w, weight, x[v].w);
+    }
+  }
+#pragma unroll
+  for (int v = 0; v < VECS; ++v) sums[who][at + v * LANES] = x[v];
+  if (at == 0) share[who] = l;
+  __syncthreads();
+  if (threadIdx.x < DP / 4) {
+    float all = 0;
+    float4 y = make_float4(0, 0, 0, 0);
+    for (int i = 0; i < AT_ONCE; ++i) {
+      const float4 s = sums[i][threadIdx.x];
+      all += share[i];
+      y.x += s.x, y.y += s.y, y.z += s.z, y.w += s.w;
+    }
+    const int d = threadIdx.x * 4;
+    if (d < a.D) {
+      T* out = static_cast<T*>(a.out) + ((size_t)join.x * a.Hq + (size_t)(join.y / per) * a.group + head0 + row) * a.D + d;
+      const float z[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) out[k] = narrow<T>(top == -INFINITY ? 0.0f : __fdiv_rn(z[k], all));
+    }
+  }
+}
+
+__device__ __forceinline__ uint32_t shared_address(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+// 16 bytes to shared memory, or 16 zeros
+__device__ __forceinline__ void copy16(uint32_t to, const void* from, bool there) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(there ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void commit_copies() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void wait_copies() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// The block number of a token and its slot's place in the block, read ahead of the copies.
+struct Ahead {
+  int page;
+  uint32_t inside;
+};
+template <int TILE, int TOKENS>
+__device__ __forceinline__ Ahead look_ahead(const AttentionArgs& a, const Cursor<TILE>& c, int warp, int lane) {
+  Ahead r{-2, 0};                              // -2: no token
+  if (c.left <= 0 || lane >= TOKENS) return r;
+  const uint32_t p = (uint32_t)c.span.first + (uint32_t)c.tile * TILE + warp * TOKENS + lane;
+  if (p >= (uint32_t)c.span.end) return r;
+  const uint32_t page = p / a.block;
+  r.page = a.table[(size_t)c.b * a.W + page];
+  if (r.page < 0) r.page = -1;                 // (no block: reported when its turn comes)
+  r.inside = p - page * a.block.d;
+  return r;
+}
+
+// Asks for the keys and values of a warp's tokens of a tile; returns which of them there are.  A row of DP elements is
+// kept as 16-byte chunks, chunk c of row r at c ^ SWIZZLE(r).
+template <class T, int DP, int TOKENS, int TILE, class SwizzleK, class SwizzleV>
+__device__ __forceinline__ uint32_t ask_for(const AttentionArgs& a, const Cursor<TILE>& c, Ahead ahead, uint32_t stage, int lane, SwizzleK sk, SwizzleV sv) {
+  constexpr int PER = 16 / sizeof(T), CHUNKS = DP / PER, ACROSS = CHUNKS < 32 ? CHUNKS : 32, ROWS = 32 / ACROSS;
+  const long long slot = (long long)ahead.page * a.block.d + ahead.inside;
+  const bool there = ahead.page >= 0 && slot < a.S;
+  if (ahead.page != -2 && !there) raise_index(a.report);
+  const uint32_t have = __ballot_sync(~0u, there);
+  const long long offset = there ? (slot * a.Hk + c.unit / (a.units / a.Hk)) * a.D : 0;
+#pragma unroll
+  for (int r = 0; r < TOKENS; r += ROWS) {
+    const int row = r + lane / ACROSS;
+    const long long from = __shfl_sync(~0u, offset, row);
+    const bool is = have >> row & 1;
+#pragma unroll
+    for (int k = 0; k < CHUNKS; k += ACROSS) {
+      const int chunk = k + lane % ACROSS;
+      const bool want = is && chunk * PER < a.D;
+      const long long at = want ? from + chunk * PER : 0;
+      copy16(stage + (row * CHUNKS + (chunk ^ sk(row))) * 16, static_cast<const T*>(a.keys) + at, want);
+      copy16(stage + ((TOKENS + row) * CHUNKS + (chunk ^ sv(row))) * 16, static_cast<const T*>(a.values) + at, want);
+    }
+  }
+  return have;
+}
+
+// ---- 16-bit types: matrix instructions ------------------------------------------------------------------------------
+
+template <class T> struct Half;
+template <> struct Half<__half> {
+  // weights are held as 2^(s - m + 12), so that the smallest that count are no subnormal numbers of the type
+  static constexpr float kRaise = 12.0f;
+  static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
+    const __half2 v = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&v);
+  }
+  static __device__ __forceinline__ float2 unpack(uint32_t v) { return __half22float2(*reinterpret_cast<const __half2*>(&v)); }
+  static __device__ __forceinline__ void mma(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+  }
+};
+template <> struct Half<__nv_bfloat16> {
+  static constexpr float kRaise = 0.0f;
+  static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&v);
+  }
+  static __device__ __forceinline__ float2 unpack(uint32_t v) { return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xFFFF0000u)); }
+  static __device__ __forceinline__ void mma(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+  }
+};
+
+__device__ __forceinline__ void load_matrices(uint32_t* r, uint32_t at) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+}
+__device__ __forceinline__ void load_matrices_transposed(uint32_t* r, uint32_t at) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+}
+__device__ __forceinline__ uint32_t transpose_matrix(uint32_t v) {
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  return r;
+}
+
+template <int DP, int NT>
+struct HalfShape {
+  static constexpr int kTokens = 16, kTile = kWarps * kTokens, kRows = 8 * NT, kPitch = DP + 4;
+  static constexpr int kStageBytes = 2 * kTokens * DP * 2;
+  // stages and resident blocks per SM: as many as 227 KB hold
+  static constexpr int kStages = DP == 64 ? 4 : NT == 2 ? 2 : 3;
+  static constexpr int kResident = DP == 256 ? 1 : DP == 64 && NT == 1 ? 3 : 2;
+  static constexpr int kSumBytes = kWarps * kRows * kPitch * 4;
+  static constexpr int kShared = kWarps * kStages * kStageBytes + kSumBytes;
+};
+
+// Scores as keys x queries (16 tokens x 8 heads, products of 16-bit values exact, sums in 32 bits), weighted values as
+// values^T x weights (16 dimensions x 8 heads): the heads are the eight columns of a matrix instruction both times, and a
+// lane's scores, maxima and sums belong to the same two heads, so that nothing is exchanged to rescale them.  The weights
+// go from one shape to the other by transposing 8 x 8 matrices, as two 16-bit parts each (value and remainder), which
+// holds them to 2^-17 (bf16) or 2^-22 (fp16): one part alone would cost up to 2^-9 of sum w |v|, more than the rounding
+// of the result where values cancel, and the second product is hidden behind the loads.
+template <class T, int DP, int NT>
+__global__ void __launch_bounds__(kThreads) k_attention_half(AttentionArgs a) {
+  using H = Half<T>;
+  using S = HalfShape<DP, NT>;
+  extern __shared__ __align__(128) unsigned char shared[];
+  __shared__ long long scan[kWarps];
+  __shared__ Place place;
+  __shared__ float ml[2 * kWarps * S::kRows];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  if (a.parts) cudaTriggerProgrammaticLaunchCompletion();
+  float* sums = reinterpret_cast<float*>(shared + kWarps * S::kStages * S::kStageBytes);
+  Cursor<S::kTile> c = find_place<T, S::kTile>(a, &place, scan);
+  int4 join = make_int4(-1, 0, 0, 0);
+  if (c.left <= 0) {
+    if (a.parts && threadIdx.x == 0) a.joins[blockIdx.x] = join;
+    return;
+  }
+  const uint32_t ring = shared_address(shared) + warp * S::kStages * S::kStageBytes;
+  const auto swizzle = [](int row) { return row & 7; };
+  // where this lane's rows of the 8 x 8 matrices start: tokens 0-7 | 8-15 by dimensions 0-7 | 8-15
+  const int k_row = (lane & 7) + (lane >> 3 & 1) * 8, k_half = lane >> 4;
+  const int v_row = (lane & 7) + (lane >> 4) * 8, v_half = lane >> 3 & 1;
+
+  Cursor<S::kTile> next = c;
+  Ahead ahead = look_ahead<S::kTile, S::kTokens>(a, next, warp, lane);
+  uint32_t have[S::kStages];
+#pragma unroll
+  for (int s = 0; s < S::kStages - 1; ++s) {
+    have[s] = 0;
+    if (next.left > 0) {
+      have[s] = ask_for<T, DP, S::kTokens>(a, next, ahead, ring + s * S::kStageBytes, lane, swizzle, swizzle);
+      next.advance(a);
+      ahead = look_ahead<S::kTile, S::kTokens>(a, next, warp, lane);
+    }
+    commit_copies();
+  }
+  uint32_t q[NT][DP / 16][2];
+  float o[NT][DP / 16][4], m[NT][2], l[NT][2];
+  bool fresh = true, from_start = c.tile == 0;
+  int stage = 0;
+  while (c.left > 0) {
+    if (fresh) {                               // a unit's queries: column n of B is head n, its rows are dimensions
+      fresh = false;
+      const int per = a.units / a.Hk, head0 = c.unit % per * S::kRows, kv = c.unit / per;
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        const int head = head0 + n * 8 + (lane >> 2);
+        const uint32_t* from = reinterpret_cast<const uint32_t*>(static_cast<const T*>(a.q) + ((size_t)c.b * a.Hq + (size_t)kv * a.group + head) * a.D) + (lane & 3);
+#pragma unroll
+        for (int k = 0; k < DP / 16; ++k) {
+          q[n][k][0] = head < a.group && k * 16 < a.D ? from[k * 8] : 0;
+          q[n][k][1] = head < a.group && k * 16 + 8 < a.D ? from[k * 8 + 4] : 0;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[n][k][i] = 0;
+        }
+        m[n][0] = m[n][1] = -INFINITY;
+        l[n][0] = l[n][1] = 0;
+      }
+    }
+    // the tile S::kStages - 1 further on
+    uint32_t got = 0;
+    {
+      int to = stage + S::kStages - 1;
+      if (to >= S::kStages) to -= S::kStages;
+      if (next.left > 0) {
+        got = ask_for<T, DP, S::kTokens>(a, next, ahead, ring + to * S::kStageBytes, lane, swizzle, swizzle);
+        next.advance(a);
+        ahead = look_ahead<S::kTile, S::kTokens>(a, next, warp, lane);
+      }
+      commit_copies();
+    }
+    wait_copies<S::kStages - 1>();
+    __syncwarp();
+    const uint32_t valid = have[0];
+#pragma unroll
+    for (int s = 0; s + 1 < S::kStages - 1; ++s) have[s] = have[s + 1];
+    have[S::kStages - 2] = got;
+    if (valid) {
+      const uint32_t keys = ring + stage * S::kStageBytes, values = keys + S::kTokens * DP * 2;
+      float s[NT][4];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0;
+#pragma unroll
+      for (int k = 0; k < DP / 16; ++k) {
+        uint32_t f[4];
+        load_matrices(f, keys + k_row * DP * 2 + (((k * 2 + k_half) ^ (k_row & 7)) << 4));
+#pragma unroll
+        for (int n = 0; n < NT; ++n) H::mma(s[n], f, q[n][k][0], q[n][k][1]);
+      }
+      const bool low = valid >> (lane >> 2) & 1, high = valid >> ((lane >> 2) + 8) & 1;
+      uint32_t w_hi[NT][2], w_lo[NT][2];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[n][i] = (i < 2 ? low : high) ? s[n][i] * a.scale_log2 : -INFINITY;
+        float top[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          top[i] = fmaxf(low ? fmaxf(s[n][i], -FLT_MAX) : -INFINITY, high ? fmaxf(s[n][i + 2], -FLT_MAX) : -INFINITY);
+#pragma unroll
+          for (int d = 4; d < 32; d <<= 1) top[i] = fmaxf(top[i], __shfl_xor_sync(~0u, top[i], d));
+          top[i] = fmaxf(top[i], m[n][i]);
+        }
+        if (__any_sync(~0u, top[0] > m[n][0] || top[1] > m[n][1])) {
+          const float f0 = exp2f(m[n][0] - top[0]), f1 = exp2f(m[n][1] - top[1]);     // (valid: the new maxima are finite, or above)
+#pragma unroll
+          for (int k = 0; k < DP / 16; ++k) o[n][k][0] *= f0, o[n][k][1] *= f1, o[n][k][2] *= f0, o[n][k][3] *= f1;
+          l[n][0] *= f0, l[n][1] *= f1;
+          m[n][0] = top[0], m[n][1] = top[1];
+        }
+        float w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = exp2f(s[n][i] - m[n][i & 1] + H::kRaise);
+        l[n][0] += w[0] + w[2];
+        l[n][1] += w[1] + w[3];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const uint32_t hi = H::pack(w[2 * i], w[2 * i + 1]);
+          const float2 back = H::unpack(hi);
+          const uint32_t lo = H::pack(w[2 * i] - back.x, w[2 * i + 1] - back.y);
+          w_hi[n][i] = transpose_matrix(hi);
+          w_lo[n][i] = transpose_matrix(lo);
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < DP / 16; ++k) {
+        uint32_t f[4];
+        load_matrices_transposed(f, values + v_row * DP * 2 + (((k * 2 + v_half) ^ (v_row & 7)) << 4));
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          H::mma(o[n][k], f, w_hi[n][0], w_hi[n][1]);
+          H::mma(o[n][k], f, w_lo[n][0], w_lo[n][1]);
+        }
+      }
+    }
+    __syncwarp();                              // the stage may be filled again
+    if (++stage == S::kStages) stage = 0;
+    const bool to_end = c.tile + 1 == c.tiles;
+    if (to_end || c.left == 1) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+#pragma unroll
+          for (int d = 4; d < 32; d <<= 1) l[n][i] += __shfl_xor_sync(~0u, l[n][i], d);
+          const int row = n * 8 + (lane & 3) * 2 + i;
+          if (lane < 4) {
+            ml[warp * S::kRows + row] = m[n][i];
+            ml[(kWarps + warp) * S::kRows + row] = l[n][i];
+          }
+          float* to = sums + (size_t)(warp * S::kRows + row) * S::kPitch + (lane >> 2);
+#pragma unroll
+          for (int k = 0; k < DP / 16; ++k) to[k * 16] = o[n][k][i], to[k * 16 + 8] = o[n][k][i + 2];
+        }
+      }
+      __syncthreads();
+      finish_unit<T, DP, S::kRows, S::kPitch, S::kTile>(a, c, from_start, to_end, sums, ml);
+      if (from_start && !to_end) {
+        const long long unit_end = run_start(blockIdx.x + 1, place.total, place.blocks) - 1 - c.tile + c.tiles;   // in tiles of the list
+        join = make_int4(c.b, c.unit, (int)((unit_end * place.blocks - 1) / place.total), 0);
+      }
+      __syncthreads();
+      fresh = from_start = true;
+    }
+    c.advance(a);
+  }
+  wait_copies<0>();
+  if (a.parts && threadIdx.x == 0) a.joins[blockIdx.x] = join;
+}
+
+// ---- fp32 --------------------------------------------------------------------------------------------------------------
+
+template <int DP>
+struct FloatShape {
+  static constexpr int kTokens = 8, kTile = kWarps * kTokens, kRows = 8, kPitch = DP;
+  static constexpr int kStageBytes = 2 * kTokens * DP * 4;
+  static constexpr int kStages = DP == 64 ? 3 : 2;
+  static constexpr int kResident = DP == 256 ? 1 : DP == 128 ? 2 : 3;
+  static constexpr int kSumBytes = kWarps * kRows * kPitch * 4, kQueryBytes = kRows * DP * 4;
+  static constexpr int kShared = kWarps * kStages * kStageBytes + kSumBytes + kQueryBytes;
+};
+
+// The same walk with 32-bit multiplications and additions, eight heads at a time.  Scores: lane 4 t + p has every fourth
+// chunk of token t's key, each chunk used for eight heads; their sums are scattered over the four lanes, two heads to a
+// lane.  Values: a lane has four dimensions of all eight heads.
+template <int DP>
+__global__ void __launch_bounds__(kThreads) k_attention_float(AttentionArgs a) {
+  using S = FloatShape<DP>;
+  constexpr int CHUNKS = DP / 4, SPLIT = CHUNKS < 32 ? 32 / CHUNKS : 1, VECS = CHUNKS / 32 > 1 ? CHUNKS / 32 : 1;
+  extern __shared__ __align__(128) unsigned char shared[];
+  __shared__ long long scan[kWarps];
+  __shared__ Place place;
+  __shared__ float ml[2 * kWarps * S::kRows];
+  __shared__ __align__(16) float weights[kWarps][8][8], falls[kWarps][8];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  if (a.parts) cudaTriggerProgrammaticLaunchCompletion();
+  float* sums = reinterpret_cast<float*>(shared + kWarps * S::kStages * S::kStageBytes);
+  float* query = sums + kWarps * S::kRows * S::kPitch;
+  Cursor<S::kTile> c = find_place<float, S::kTile>(a, &place, scan);
+  int4 join = make_int4(-1, 0, 0, 0);
+  if (c.left <= 0) {
+    if (a.parts && threadIdx.x == 0) a.joins[blockIdx.x] = join;
+    return;
+  }
+  const unsigned char* ring = shared + warp * S::kStages * S::kStageBytes;
+  const uint32_t ring_at = shared_address(ring);
+  const auto swizzle_keys = [](int row) { return (row & 1) << 2; };
+  const auto plain = [](int) { return 0; };
+  const int token = lane >> 2, part = lane & 3;
+  const int head = (part & 1) * 4 + (part >> 1) * 2;         // and the one behind it: the two that this lane's sums end up with
+  const int chunk = lane % (CHUNKS < 32 ? CHUNKS : 32), half = lane / (CHUNKS < 32 ? CHUNKS : 32);
+
+  Cursor<S::kTile> next = c;
+  Ahead ahead = look_ahead<S::kTile, S::kTokens>(a, next, warp, lane);
+  uint32_t have[S::kStages];
+#pragma unroll
+  for (int s = 0; s < S::kStages - 1; ++s) {
+    have[s] = 0;
+    if (next.left > 0) {
+      have[s] = ask_for<float, DP, S::kTokens>(a, next, ahead, ring_at + s * S::kStageBytes, lane, swizzle_keys, plain);
+      next.advance(a);
+      ahead = look_ahead<S::kTile, S::kTokens>(a, next, warp, lane);
+    }
+    commit_copies();
+  }
+  float o[8][VECS][4], m[2], l[2];
+  bool fresh = true, from_start = c.tile == 0;
+  int stage = 0;
+  while (c.left > 0) {
+    if (fresh) {
+      fresh = false;
+      const int per = a.units / a.Hk, head0 = c.unit % per * S::kRows, kv = c.unit / per;
+      for (int i = threadIdx.x; i < 8 * DP; i += kThreads) {
+        const int h = i / DP, d = i % DP;
+        query[i] = head0 + h < a.group && d < a.D ? static_cast<const float*>(a.q)[((size_t)c.b * a.Hq + (size_t)kv * a.group + head0 + h) * a.D + d] : 0.0f;
+      }
+#pragma unroll
+      for (int h = 0; h < 8; ++h)
+#pragma unroll
+        for (int v = 0; v < VECS; ++v) o[h][v][0] = o[h][v][1] = o[h][v][2] = o[h][v][3] = 0;
+      m[0] = m[1] = -INFINITY;
+      l[0] = l[1] = 0;
+      __syncthreads();
+    }
+    uint32_t got = 0;
+    {
+      int to = stage + S::kStages - 1;
+      if (to >= S::kStages) to -= S::kStages;
+      if (next.left > 0) {
+        got = ask_for<float, DP, S::kTokens>(a, next, ahead, ring_at + to * S::kStageBytes, lane, swizzle_keys, plain);
+        next.advance(a);
+        ahead = look_ahead<S::kTile, S::kTokens>(a, next, warp, lane);
+      }
+      commit_copies();
+    }
+    wait_copies<S::kStages - 1>();
+    __syncwarp();
+    const uint32_t valid = have[0];
+#pragma unroll
+    for (int s = 0; s + 1 < S::kStages - 1; ++s) have[s] = have[s + 1];
+    have[S::kStages - 2] = got;
+    if (valid) {
+      const float4* keys = reinterpret_cast<const float4*>(ring + stage * S::kStageBytes) + token * CHUNKS;
+      const float4* values = reinterpret_cast<const float4*>(ring + stage * S::kStageBytes) + S::kTokens * CHUNKS;
+      float s[8];
+#pragma unroll
+      for (int h = 0; h < 8; ++h) s[h] = 0;
+#pragma unroll 4
+      for (int i = 0; i < CHUNKS / 4; ++i) {
+        const float4 k = keys[(i * 4 + part) ^ ((token & 1) << 2)];
+#pragma unroll
+        for (int h = 0; h < 8; ++h) {
+          const float4 x = reinterpret_cast<const float4*>(query)[h * CHUNKS + i * 4 + part];
+          s[h] = fmaf(k.x, x.x, fmaf(k.y, x.y, fmaf(k.z, x.z, fmaf(k.w, x.w, s[h]))));
+        }
+      }
+      float t4[4], t2[2];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float other = __shfl_xor_sync(~0u, part & 1 ? s[i] : s[i + 4], 1);
+        t4[i] = (part & 1 ? s[i + 4] : s[i]) + other;
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const float other = __shfl_xor_sync(~0u, part & 2 ? t4[i] : t4[i + 2], 2);
+        t2[i] = (part & 2 ? t4[i + 2] : t4[i]) + other;
+      }
+      const bool is = valid >> token & 1;
+      float top[2];
+      bool rises = false;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        t2[i] = is ? t2[i] * a.scale_log2 : -INFINITY;
+        top[i] = is ? fmaxf(t2[i], -FLT_MAX) : -INFINITY;
+#pragma unroll
+        for (int d = 4; d < 32; d <<= 1) top[i] = fmaxf(top[i], __shfl_xor_sync(~0u, top[i], d));
+        top[i] = fmaxf(top[i], m[i]);
+        rises = rises || top[i] > m[i];
+      }
+      rises = __any_sync(~0u, rises);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const float fall = exp2f(m[i] - top[i]);
+        const float w = exp2f(t2[i] - top[i]);
+        l[i] = fmaf(l[i], fall, w);
+        m[i] = top[i];
+        weights[warp][head + i][token] = w;
+        if (token == 0) falls[warp][head + i] = fall;
+      }
+      __syncwarp();
+#pragma unroll
+      for (int h = 0; h < 8; ++h) {
+        if (rises) {
+          const float fall = falls[warp][h];
+#pragma unroll
+          for (int v = 0; v < VECS; ++v) o[h][v][0] *= fall, o[h][v][1] *= fall, o[h][v][2] *= fall, o[h][v][3] *= fall;
+        }
+      }
+      constexpr int QUADS = 2 / SPLIT;                       // fours of tokens that a lane goes through
+#pragma unroll
+      for (int f = 0; f < QUADS; ++f) {
+        const int t0 = (SPLIT == 2 ? half : f) * 4;
+        float4 w[8];
+#pragma unroll
+        for (int h = 0; h < 8; ++h) w[h] = *reinterpret_cast<const float4*>(&weights[warp][h][t0]);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+#pragma unroll
+          for (int v = 0; v < VECS; ++v) {
+            const float4 x = values[(t0 + t) * CHUNKS + chunk + v * 32];
+#pragma unroll
+            for (int h = 0; h < 8; ++h) {
+              const float y = t == 0 ? w[h].x : t == 1 ? w[h].y : t == 2 ? w[h].z : w[h].w;
+              o[h][v][0] = fmaf(y, x.x, o[h][v][0]), o[h][v][1] = fmaf(y, x.y, o[h][v][1]);
+              o[h][v][2] = fmaf(y, x.z, o[h][v][2]), o[h][v][3] = fmaf(y, x.w, o[h][v][3]);
+            }
+          }
+        }
+      }
+    }
+    __syncwarp();
+    if (++stage == S::kStages) stage = 0;
+    const bool to_end = c.tile + 1 == c.tiles;
+    if (to_end || c.left == 1) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+#pragma unroll
+        for (int d = 4; d < 32; d <<= 1) l[i] += __shfl_xor_sync(~0u, l[i], d);
+        if (token == 0) {
+          ml[warp * S::kRows + head + i] = m[i];
+          ml[(kWarps + warp) * S::kRows + head + i] = l[i];
+        }
+      }
+#pragma unroll
+      for (int h = 0; h < 8; ++h)
+#pragma unroll
+        for (int v = 0; v < VECS; ++v) {
+          if constexpr (SPLIT == 2)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[h][v][i] += __shfl_xor_sync(~0u, o[h][v][i], 16);
+          if (half == 0)
+            *reinterpret_cast<float4*>(sums + (size_t)(warp * S::kRows + h) * S::kPitch + (chunk + v * 32) * 4) = make_float4(o[h][v][0], o[h][v][1], o[h][v][2], o[h][v][3]);
+        }
+      __syncthreads();
+      finish_unit<float, DP, S::kRows, S::kPitch, S::kTile>(a, c, from_start, to_end, sums, ml);
+      if (from_start && !to_end) {
+        const long long unit_end = run_start(blockIdx.x + 1, place.total, place.blocks) - 1 - c.tile + c.tiles;
+        join = make_int4(c.b, c.unit, (int)((unit_end * place.blocks - 1) / place.total), 0);
+      }
+      __syncthreads();
+      fresh = from_start = true;
+    }
+    c.advance(a);
+  }
+  wait_copies<0>();
+  if (a.parts && threadIdx.x == 0) a.joins[blockIdx.x] = join;
+}
+
+// ---- launches ------------------------------------------------------------------------------------------------------------
+
+AttentionArgs arguments(const ClusterLaunch& L) {
+  const int D = (int)L.op.iparam[1];
+  const int Hq = (int)L.op.shape[1] / D, Hk = slot(L, 1).C / D;
+  const bool empty = slot(L, 1).R == 0;                       // (a copy of no bytes still names an address)
+  return {report_of(L), slot(L, 0).ptr, slot(L, empty ? 0 : 1).ptr, slot(L, empty ? 0 : 2).ptr, slot_ptr<int>(L, 3), slot_ptr<int>(L, 4), result_ptr<void>(L),
+          (int)L.op.shape[0], slot(L, 3).C, slot(L, 1).R, Hq, Hk, D, (int)std::min<int64_t>(L.op.iparam[2], 0x7FFFFFFF),
+          Hk > 0 ? Hq / Hk : 0, 0, (float)(L.op.fparam[0] * 1.4426950408889634), divisor((uint32_t)L.op.iparam[0]), nullptr, nullptr};
+}
+
+// Blocks of the grid, and whether a unit may be split: never if no request can have more than a tile.
+template <class S>
+int grid_of(AttentionArgs& a, bool& splits) {
+  a.units = a.Hk * ((a.group + S::kRows - 1) / S::kRows);
+  const long long room = (long long)a.W * a.block.d;
+  const long long tiles = std::max<long long>((room + S::kTile - 1) / S::kTile, 1) * a.B * a.units;
+  splits = room > S::kTile;
+  return (int)std::min<long long>(tiles, (long long)sm_count() * S::kResident);
+}
+
+template <class S, int DP>
+int64_t scratch_of(AttentionArgs a) {
+  bool splits;
+  const int64_t grid = grid_of<S>(a, splits);
+  return splits ? grid * (16 + 2 * S::kRows * (DP + 2) * 4) : 0;
+}
+
+template <class T, int DP, class S, class K>
+int run(const ClusterLaunch& L, K kernel, std::atomic<uint64_t>& allowed) {
+  AttentionArgs a = arguments(L);
+  bool splits;
+  const int grid = grid_of<S>(a, splits);
+  if (splits) {
+    a.joins = reinterpret_cast<int4*>(L.scratch);
+    a.parts = reinterpret_cast<float*>(a.joins + grid);
+  }
+  const int rc = allow_shared(kernel, S::kShared, allowed);
+  if (rc != ACC_OK) return rc;
+  kernel<<<grid, kThreads, S::kShared, L.stream>>>(a);
+  if (!splits) return launched();
+  // the joining kernel is launched early and waits for the first one on the device
+  cudaLaunchConfig_t config{};
+  config.gridDim = dim3(grid, std::min(S::kRows, a.group));
+  config.blockDim = dim3(256);
+  config.stream = L.stream;
+  cudaLaunchAttribute early{};
+  early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  early.val.programmaticStreamSerializationAllowed = 1;
+  config.attrs = &early;
+  config.numAttrs = 1;
+  ++L.extra_launches;
+  const cudaError_t e = cudaLaunchKernelEx(&config, k_join<T, DP, S::kRows>, a);
+  return e == cudaSuccess ? launched() : set_error(ACC_ERR_CUDA, "kernel launch failed: %s", cudaGetErrorString(cudaGetLastError()));
+}
+
+// Calls f(shape, DP, pointer to the kernel, flags) for the kernel that a launch takes: heads padded to 64, 128 or 256
+// elements; for 16-bit types sixteen heads at a time where a key head has more than eight (a head of up to 128 elements:
+// beyond, the registers do not hold them).
+template <class F>
+auto choose(const ClusterLaunch& L, F f) {
+  const int D = (int)L.op.iparam[1];
+  const int Hk = slot(L, 1).C / D, group = Hk > 0 ? (int)L.op.shape[1] / D / Hk : 0;
+  const bool wide = group > 8;
+  if (L.op.dtype == ACC_F32) {
+    if (D <= 64) return f(float{}, std::integral_constant<int, 64>{}, FloatShape<64>{}, k_attention_float<64>);
+    if (D <= 128) return f(float{}, std::integral_constant<int, 128>{}, FloatShape<128>{}, k_attention_float<128>);
+    return f(float{}, std::integral_constant<int, 256>{}, FloatShape<256>{}, k_attention_float<256>);
+  }
+  const auto half = [&](auto t) {
+    using T = decltype(t);
+    if (D <= 64) return wide ? f(t, std::integral_constant<int, 64>{}, HalfShape<64, 2>{}, k_attention_half<T, 64, 2>)
+                             : f(t, std::integral_constant<int, 64>{}, HalfShape<64, 1>{}, k_attention_half<T, 64, 1>);
+    if (D <= 128) return wide ? f(t, std::integral_constant<int, 128>{}, HalfShape<128, 2>{}, k_attention_half<T, 128, 2>)
+                              : f(t, std::integral_constant<int, 128>{}, HalfShape<128, 1>{}, k_attention_half<T, 128, 1>);
+    return f(t, std::integral_constant<int, 256>{}, HalfShape<256, 1>{}, k_attention_half<T, 256, 1>);
+  };
+  return L.op.dtype == ACC_F16 ? half(__half{}) : half(__nv_bfloat16{});
+}
+
+bool nothing(const ClusterLaunch& L) { return L.op.shape[0] == 0 || L.op.shape[1] == 0; }
+
+int64_t attention_scratch(const ClusterLaunch& L) {
+  if (nothing(L)) return 0;
+  return choose(L, [&](auto, auto dp, auto shape, auto) { return scratch_of<decltype(shape), decltype(dp)::value>(arguments(L)); });
 }
 
 int launch_attention(const ClusterLaunch& L) {
-  const int D = (int)L.op.iparam[1];
-  AttentionArgs a{report_of(L), slot(L, 0).ptr, slot(L, 1).ptr, slot(L, 2).ptr, slot_ptr<int>(L, 3), slot_ptr<int>(L, 4), result_ptr<void>(L),
-                  (int)L.op.shape[0], slot(L, 3).C, slot(L, 1).R, (int)L.op.shape[1] / D, slot(L, 1).C / D, D,
-                  (int)std::min<int64_t>(L.op.iparam[2], 0x7FFFFFFF), (float)L.op.fparam[0], divisor((uint32_t)L.op.iparam[0])};
-  if (a.B == 0 || a.Hq == 0) return ACC_OK;
-  const dim3 grid(a.B, a.Hq);
-  if (L.op.dtype == ACC_F32) k_attention_simple<float><<<grid, 128, 0, L.stream>>>(a);
-  else if (L.op.dtype == ACC_F16) k_attention_simple<__half><<<grid, 128, 0, L.stream>>>(a);
-  else k_attention_simple<__nv_bfloat16><<<grid, 128, 0, L.stream>>>(a);
-  return launched();
+  if (nothing(L)) return ACC_OK;
+  return choose(L, [&](auto t, auto dp, auto shape, auto kernel) {
+    static std::atomic<uint64_t> allowed{0};
+    return run<decltype(t), decltype(dp)::value, decltype(shape)>(L, kernel, allowed);
+  });
 }
 
-const Register attention(ACC_PAGED_ATTENTION, "k_attention", no_scratch, launch_attention);
+const Register attention(ACC_PAGED_ATTENTION, "k_attention", attention_scratch, launch_attention);
 
 }  // namespace
 }  // namespace ops

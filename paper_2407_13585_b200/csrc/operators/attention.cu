@@ -33,8 +33,19 @@ struct AttentionArgs {
   float scale_log2;       // log2(e) scale
   Divisor block;
   float* parts;           // two records of sums per block of the grid; null: no unit is split
-  int4* joins;            // per block of the grid: {request, unit, last block of it, 0} of the split unit that starts there
+  int grid, join_rows;    // blocks of the grid; heads that a block of the joining kernel takes
+  // {request, unit, first block, last block} of split units, -1 for none: by unit (request * units + unit) where there are no
+  // more units than blocks, else by the block that a unit starts in
+  int4* joins;
+  bool by_unit;
 };
+
+// 2^x to 2^-22; results below 2^-126, which no sum would notice, are zeros.
+__device__ __forceinline__ float power2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
 
 constexpr int kWarps = 4, kThreads = kWarps * 32;
 
@@ -80,7 +91,17 @@ struct Place {
   int b;                     // the request that the run starts in
   long long b_start;         // tiles before that request
 };
-__device__ __forceinline__ long long run_start(int block, long long total, int blocks) { return (long long)block * total / blocks; }
+__device__ __forceinline__ long long run_start(int block, long long total, int blocks) {
+  if (total < 1 << 20) return (uint32_t)block * (uint32_t)total / (uint32_t)blocks;     // (at most 2^10 blocks)
+  return (long long)block * total / blocks;
+}
+
+// What the joining kernel needs of the unit whose start this block has and whose end it has not.
+template <int TILE>
+__device__ __forceinline__ int4 join_of(const AttentionArgs& a, const Cursor<TILE>& c, const Place& place) {
+  const long long unit_end = run_start(blockIdx.x + 1, place.total, place.blocks) - 1 - c.tile + c.tiles;     // in tiles of the list
+  return make_int4(c.b, c.unit, blockIdx.x, (int)((unit_end * place.blocks - 1) / place.total));
+}
 
 // Where this block's run of the list starts.  Every thread adds up a share of the requests; requests without tokens get
 // their zeros here, spread over the grid.
@@ -129,6 +150,8 @@ __device__ Cursor<TILE> find_place(const AttentionArgs& a, Place* shared, long l
     const Span s = span_of(a, r);
     if (s.first < s.end) continue;
     for (int d = threadIdx.x; d < a.Hq * a.D; d += kThreads) static_cast<T*>(a.out)[(size_t)r * a.Hq * a.D + d] = narrow<T>(0.0f);
+    if (a.parts && a.by_unit)
+      for (int u = threadIdx.x; u < a.units; u += kThreads) a.joins[(size_t)r * a.units + u] = make_int4(-1, 0, 0, 0);
   }
   __syncthreads();
   Cursor<TILE> c{};
@@ -136,22 +159,35 @@ __device__ Cursor<TILE> find_place(const AttentionArgs& a, Place* shared, long l
   c.b = shared->b;
   c.enter(a);
   const long long inside = start - shared->b_start;
-  c.unit = (int)(inside / c.tiles);
+  c.unit = inside <= 0x7FFFFFFF ? (int)((uint32_t)inside / (uint32_t)c.tiles) : (int)(inside / c.tiles);
   c.tile = (int)(inside - (long long)c.unit * c.tiles);
   c.left = end - start;
   return c;
 }
 
-// The four warps' sums of a unit's tiles [from, ...) that this block had, in shared memory: sums[warp][row][pitch], their
-// maxima and weights in ml[0][warp][row], ml[1][warp][row].  Written out if they are the whole unit, else to scratch.
-// The weights of a row without any token have the maximum -infinity; with tokens it is at least -FLT_MAX.
-template <class T, int DP, int ROWS, int PITCH, int TILE>
-__device__ __forceinline__ void finish_unit(const AttentionArgs& a, const Cursor<TILE>& c, bool from_start, bool to_end,
-                                            const float* sums, const float* ml) {
-  const int head0 = c.unit % (a.units / a.Hk) * ROWS, kv = c.unit / (a.units / a.Hk);
+// Where the sums of block `block` go that does not finish a unit: record 1 if it started the unit, record 0 if it goes on
+// with it.  A record is one row of sums for every head of the unit (WAYS x ROWS x DP), its maxima and weights apart.
+template <int DP, int HEADS>
+struct Records {
+  float *sums, *tops, *weights;
+  __host__ __device__ static constexpr size_t bytes(int blocks) { return (size_t)blocks * 2 * HEADS * (DP + 2) * 4; }
+  __device__ __forceinline__ Records(const AttentionArgs& a)
+      : sums(a.parts), tops(a.parts + (size_t)a.grid * 2 * HEADS * DP), weights(tops + (size_t)a.grid * 2 * HEADS) {}
+  __device__ __forceinline__ static size_t row(int block, bool started, int head) { return ((size_t)block * 2 + (started ? 1 : 0)) * HEADS + head; }
+};
+
+// In the shared sums of a warp, dimension d of row r lies at d ^ spread(r): the eight dimensions that a matrix
+// instruction's result has in a column go to banks of their own for each of the four columns written together.
+__device__ __forceinline__ int spread(int row) { return (row >> 1 & 3) << 3; }
+
+// The four warps' sums over the tokens of one unit, sums[warp * stride + row * DP + ...], their maxima and weights in
+// ml[0][warp][row], ml[1][warp][row].  Written out if they are the whole unit, else to scratch.  A row without any token
+// has the maximum -infinity; with tokens it is at least -FLT_MAX.
+template <class T, int DP, int ROWS, bool SPREAD>
+__device__ __forceinline__ void finish_unit(const AttentionArgs& a, int b, int kv, int head0, bool from_start, bool to_end, const float* sums, int stride,
+                                            const float* ml) {
   const int rows = min(ROWS, a.group - head0);
   const bool whole = from_start && to_end;
-  float* part = a.parts + (size_t)(blockIdx.x * 2 + (from_start ? 1 : 0)) * ROWS * (DP + 2);
   for (int i = threadIdx.x; i < rows * (DP / 4); i += kThreads) {
     const int row = i / (DP / 4), d = i % (DP / 4) * 4;
     float top = -INFINITY;
@@ -161,90 +197,143 @@ __device__ __forceinline__ void finish_unit(const AttentionArgs& a, const Cursor
     float l = 0, x[4] = {0, 0, 0, 0};
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) {
-      const float weight = exp2f(ml[w * ROWS + row] - ref);
-      const float4 s = *reinterpret_cast<const float4*>(sums + (size_t)(w * ROWS + row) * PITCH + d);
+      const float weight = power2(ml[w * ROWS + row] - ref);
+      const float4 s = *reinterpret_cast<const float4*>(sums + (size_t)w * stride + row * DP + (SPREAD ? d ^ spread(row) : d));
       l = fmaf(ml[(kWarps + w) * ROWS + row], weight, l);
       x[0] = fmaf(s.x, weight, x[0]), x[1] = fmaf(s.y, weight, x[1]), x[2] = fmaf(s.z, weight, x[2]), x[3] = fmaf(s.w, weight, x[3]);
     }
     if (whole) {
       if (d >= a.D) continue;
-      T* out = static_cast<T*>(a.out) + ((size_t)c.b * a.Hq + (size_t)kv * a.group + head0 + row) * a.D + d;
+      T* out = static_cast<T*>(a.out) + ((size_t)b * a.Hq + (size_t)kv * a.group + head0 + row) * a.D + d;
 #pragma unroll
       for (int k = 0; k < 4; ++k) out[k] = narrow<T>(top == -INFINITY ? 0.0f : __fdiv_rn(x[k], l));
     } else {
-      *reinterpret_cast<float4*>(part + row * DP + d) = make_float4(x[0], x[1], x[2], x[3]);
+      const Records<DP, ROWS> to(a);
+      const size_t at = to.row(blockIdx.x, from_start, row);
+      *reinterpret_cast<float4*>(to.sums + at * DP + d) = make_float4(x[0], x[1], x[2], x[3]);
       if (d == 0) {
-        part[ROWS * DP + row] = top;
-        part[ROWS * DP + ROWS + row] = l;
+        to.tops[at] = top;
+        to.weights[at] = l;
       }
     }
   }
 }
 
-// Sums of a split unit, one row of heads to a block: maxima first, then the records, four dimensions to a lane.
-template <class T, int DP, int ROWS>
-__global__ void __launch_bounds__(256) k_join(AttentionArgs a) {
-  constexpr int LANES = DP / 4 < 32 ? DP / 4 : 32;         // lanes that share a record's row
-  constexpr int VECS = DP / 4 / LANES, AT_ONCE = 256 / LANES;
-  __shared__ float tops[8], share[AT_ONCE];
-  __shared__ float4 sums[AT_ONCE][LANES * VECS];
+// Adds up the records of a split unit.  Few records: a warp to a head, a lane to four dimensions.  Many: the block's warps
+// share the records of 32 dimensions of a head, which a lane in eight reads four of; a block to each of these pieces where
+// units are few (a.join_rows = 1), else one block to eight heads.
+constexpr int kJoinThreads = 256, kJoinWarps = kJoinThreads / 32, kManyRecords = 16, kMaxGrid = 1024, kPiece = 32;
+template <class T, int DP, int ROWS, int WAYS>
+__global__ void __launch_bounds__(kJoinThreads) k_join(AttentionArgs a) {
+  constexpr int HEADS = ROWS * WAYS, VECS = (DP / 4 + 31) / 32;
+  __shared__ float weight[kMaxGrid];
+  __shared__ float tops[kJoinWarps], shares[kJoinWarps];
+  __shared__ float4 sums[kJoinWarps][kPiece / 4];
   cudaGridDependencySynchronize();
   const int4 join = a.joins[blockIdx.x];
   if (join.x < 0) return;
-  const int per = a.units / a.Hk, head0 = join.y % per * ROWS, row = blockIdx.y;
-  if (row >= a.group - head0) return;
-  const int n = join.z - (int)blockIdx.x + 1;
-  constexpr size_t RECORD = (size_t)ROWS * (DP + 2);
-  const auto record = [&](int i) { return a.parts + ((size_t)(blockIdx.x + i) * 2 + (i == 0 ? 1 : 0)) * RECORD; };
+  const int per = a.units / (a.Hk / WAYS), head0 = join.y % per * ROWS;
+  const int n = join.w - join.z + 1;
+  const Records<DP, HEADS> from(a);
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  float top = -INFINITY;
-  for (int i = threadIdx.x; i < n; i += 256) top = fmaxf(top, record(i)[ROWS * DP + row]);
+  const int r0 = blockIdx.y * a.join_rows;
+  const auto at = [&](int i, int h) { return from.row(join.z + i, i == 0, h); };
+  const auto add = [&](float4& y, float w, const float4& s) { y.x = fmaf(s.x, w, y.x), y.y = fmaf(s.y, w, y.y), y.z = fmaf(s.z, w, y.z), y.w = fmaf(s.w, w, y.w); };
+  const auto write = [&](int h, int d, const float4& y, float l, float top) {
+    if (d >= a.D) return;
+    const int kv = join.y / per * WAYS + h / ROWS;
+    T* out = static_cast<T*>(a.out) + ((size_t)join.x * a.Hq + (size_t)kv * a.group + head0 + h % ROWS) * a.D + d;
+    const float z[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
-  for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
-  if (lane == 0) tops[warp] = top;
-  __syncthreads();
+    for (int k = 0; k < 4; ++k) out[k] = narrow<T>(top == -INFINITY ? 0.0f : __fdiv_rn(z[k], l));
+  };
+  if (n <= kManyRecords && a.join_rows > 1) {
+    for (int h = r0 + warp; h < r0 + a.join_rows; h += kJoinWarps) {
+      if (h % ROWS >= a.group - head0) continue;
+      const float t = lane < n ? from.tops[at(lane, h)] : -INFINITY, share = lane < n ? from.weights[at(lane, h)] : 0.0f;
+      float top = t;
 #pragma unroll
-  for (int w = 0; w < 8; ++w) top = fmaxf(top, tops[w]);
-  const float ref = top == -INFINITY ? 0.0f : top;
-  const int who = threadIdx.x / LANES, at = threadIdx.x % LANES;
-  float l = 0;
-  float4 x[VECS];
-#pragma unroll
-  for (int v = 0; v < VECS; ++v) x[v] = make_float4(0, 0, 0, 0);
+      for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
+      const float w = power2(t - (top == -INFINITY ? 0.0f : top));
+      float4 y[VECS] = {};
+      float l = 0;
 #pragma unroll 4
-  for (int i = who; i < n; i += AT_ONCE) {
-    const float* r = record(i);
-    const float weight = exp2f(r[ROWS * DP + row] - ref);
-    l = fmaf(r[ROWS * DP + ROWS + row], weight, l);
+      for (int i = 0; i < n; ++i) {
+        const float wi = __shfl_sync(~0u, w, i);
+        l = fmaf(wi, __shfl_sync(~0u, share, i), l);
 #pragma unroll
-    for (int v = 0; v < VECS; ++v) {
-      const float4 s = *reinterpret_cast<const float4*>(r + row * DP + (at + v * LANES) * 4);
-      x[v].x = fmaf(s.x, weight, x[v].x), x[v].y = fmaf(s.y, weight, x[v].y), x[v].z = fmaf(s.z, weight, x[v].z), x[v].w = fmaf(s.w, weight, x[v].w);
+        for (int v = 0; v < VECS; ++v)
+          if ((lane + 32 * v) * 4 < DP) add(y[v], wi, *reinterpret_cast<const float4*>(from.sums + at(i, h) * DP + (lane + 32 * v) * 4));
+      }
+#pragma unroll
+      for (int v = 0; v < VECS; ++v) write(h, (lane + 32 * v) * 4, y[v], l, top);
     }
+    return;
   }
+  constexpr int BATCH = 8, STEP = 4 * kJoinWarps;          // four records to a warp at a time
+  const int mine = warp * 4 + (lane >> 3);
+  for (int h = r0; h < r0 + a.join_rows; ++h) {
+    if (h % ROWS >= a.group - head0) continue;
+    for (int piece = blockIdx.z; piece < DP / kPiece; piece += gridDim.z) {
+      const int d = piece * kPiece + (lane & 7) * 4;
+      const auto load = [&](int i) { return i < n ? *reinterpret_cast<const float4*>(from.sums + at(i, h) * DP + d) : make_float4(0, 0, 0, 0); };
+      float4 ahead[BATCH];                                 // on their way while the maxima are compared
 #pragma unroll
-  for (int v = 0; v < VECS; ++v) sums[who][at + v * LANES] = x[v];
-  if (at == 0) share[who] = l;
-  __syncthreads();
-  if (threadIdx.x < DP / 4) {
-    float all = 0;
-    float4 y = make_float4(0, 0, 0, 0);
-    for (int i = 0; i < AT_ONCE; ++i) {
-      const float4 s = sums[i][threadIdx.x];
-      all += share[i];
-      y.x += s.x, y.y += s.y, y.z += s.z, y.w += s.w;
-    }
-    const int d = threadIdx.x * 4;
-    if (d < a.D) {
-      T* out = static_cast<T*>(a.out) + ((size_t)join.x * a.Hq + (size_t)(join.y / per) * a.group + head0 + row) * a.D + d;
-      const float z[4] = {y.x, y.y, y.z, y.w};
+      for (int k = 0; k < BATCH; ++k) ahead[k] = load(mine + k * STEP);
+      float top = -INFINITY;
+      for (int i = threadIdx.x; i < n; i += kJoinThreads) {
+        weight[i] = from.tops[at(i, h)];
+        top = fmaxf(top, weight[i]);
+      }
 #pragma unroll
-      for (int k = 0; k < 4; ++k) out[k] = narrow<T>(top == -INFINITY ? 0.0f : __fdiv_rn(z[k], all));
+      for (int k = 16; k > 0; k >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, k));
+      if (lane == 0) tops[warp] = top;
+      __syncthreads();
+#pragma unroll
+      for (int w = 0; w < kJoinWarps; ++w) top = fmaxf(top, tops[w]);
+      const float ref = top == -INFINITY ? 0.0f : top;
+      float l = 0;
+      for (int i = threadIdx.x; i < n; i += kJoinThreads) {
+        weight[i] = power2(weight[i] - ref);
+        l = fmaf(weight[i], from.weights[at(i, h)], l);
+      }
+#pragma unroll
+      for (int k = 16; k > 0; k >>= 1) l += __shfl_xor_sync(~0u, l, k);
+      if (lane == 0) shares[warp] = l;
+      __syncthreads();
+      float4 y = make_float4(0, 0, 0, 0);
+      for (int i0 = mine; i0 < n; i0 += BATCH * STEP) {
+        if (i0 != mine)
+#pragma unroll
+          for (int k = 0; k < BATCH; ++k) ahead[k] = load(i0 + k * STEP);
+#pragma unroll
+        for (int k = 0; k < BATCH; ++k)
+          if (i0 + k * STEP < n) add(y, weight[i0 + k * STEP], ahead[k]);
+      }
+#pragma unroll
+      for (int k = 8; k < 32; k <<= 1) {
+        y.x += __shfl_xor_sync(~0u, y.x, k), y.y += __shfl_xor_sync(~0u, y.y, k);
+        y.z += __shfl_xor_sync(~0u, y.z, k), y.w += __shfl_xor_sync(~0u, y.w, k);
+      }
+      if (lane < kPiece / 4) sums[warp][lane] = y;
+      __syncthreads();
+      if (threadIdx.x < kPiece / 4) {
+        l = 0;
+        y = make_float4(0, 0, 0, 0);
+#pragma unroll
+        for (int w = 0; w < kJoinWarps; ++w) {
+          l += shares[w];
+          add(y, 1.0f, sums[w][lane]);
+        }
+        write(h, d, y, l, top);
+      }
+      __syncthreads();
     }
   }
 }
 
 __device__ __forceinline__ uint32_t shared_address(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void copy16(uint32_t to, const void* from) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory"); }
 // 16 bytes to shared memory, or 16 zeros
 __device__ __forceinline__ void copy16(uint32_t to, const void* from, bool there) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(there ? 16 : 0) : "memory");
@@ -259,10 +348,10 @@ struct Ahead {
   uint32_t inside;
 };
 template <int TILE, int TOKENS>
-__device__ __forceinline__ Ahead look_ahead(const AttentionArgs& a, const Cursor<TILE>& c, int warp, int lane) {
+__device__ __forceinline__ Ahead look_ahead(const AttentionArgs& a, const Cursor<TILE>& c, int first, int lane) {
   Ahead r{-2, 0};                              // -2: no token
   if (c.left <= 0 || lane >= TOKENS) return r;
-  const uint32_t p = (uint32_t)c.span.first + (uint32_t)c.tile * TILE + warp * TOKENS + lane;
+  const uint32_t p = (uint32_t)c.span.first + (uint32_t)c.tile * TILE + first + lane;
   if (p >= (uint32_t)c.span.end) return r;
   const uint32_t page = p / a.block;
   r.page = a.table[(size_t)c.b * a.W + page];
@@ -272,27 +361,36 @@ __device__ __forceinline__ Ahead look_ahead(const AttentionArgs& a, const Cursor
 }
 
 // Asks for the keys and values of a warp's tokens of a tile; returns which of them there are.  A row of DP elements is
-// kept as 16-byte chunks, chunk c of row r at c ^ SWIZZLE(r).
-template <class T, int DP, int TOKENS, int TILE, class SwizzleK, class SwizzleV>
-__device__ __forceinline__ uint32_t ask_for(const AttentionArgs& a, const Cursor<TILE>& c, Ahead ahead, uint32_t stage, int lane, SwizzleK sk, SwizzleV sv) {
-  constexpr int PER = 16 / sizeof(T), CHUNKS = DP / PER, ACROSS = CHUNKS < 32 ? CHUNKS : 32, ROWS = 32 / ACROSS;
+// kept as CHUNKS chunks of 16 bytes, chunk c of row r at c ^ swizzle(r).
+template <class T, int DP, int CHUNKS, int TOKENS, int TILE, class SwizzleK, class SwizzleV>
+__device__ __forceinline__ uint32_t ask_for(const AttentionArgs& a, const Cursor<TILE>& c, Ahead ahead, uint32_t stage, int lane, int kv, SwizzleK sk, SwizzleV sv) {
+  constexpr int PER = 16 / sizeof(T), ACROSS = CHUNKS < 32 ? CHUNKS : 32, ROWS = 32 / ACROSS;
   const long long slot = (long long)ahead.page * a.block.d + ahead.inside;
   const bool there = ahead.page >= 0 && slot < a.S;
   if (ahead.page != -2 && !there) raise_index(a.report);
   const uint32_t have = __ballot_sync(~0u, there);
-  const long long offset = there ? (slot * a.Hk + c.unit / (a.units / a.Hk)) * a.D : 0;
+  // in chunks: an array of 2^31 elements has fewer than 2^30
+  const uint32_t offset = there ? (uint32_t)((slot * a.Hk + kv) * a.D / PER) : 0;
+  const uint4 *keys = static_cast<const uint4*>(a.keys), *values = static_cast<const uint4*>(a.values);
+  const bool whole = a.D == DP && have == (TOKENS == 32 ? ~0u : (1u << TOKENS) - 1);
 #pragma unroll
   for (int r = 0; r < TOKENS; r += ROWS) {
     const int row = r + lane / ACROSS;
-    const long long from = __shfl_sync(~0u, offset, row);
-    const bool is = have >> row & 1;
+    const uint32_t from = __shfl_sync(~0u, offset, row);
 #pragma unroll
     for (int k = 0; k < CHUNKS; k += ACROSS) {
       const int chunk = k + lane % ACROSS;
-      const bool want = is && chunk * PER < a.D;
-      const long long at = want ? from + chunk * PER : 0;
-      copy16(stage + (row * CHUNKS + (chunk ^ sk(row))) * 16, static_cast<const T*>(a.keys) + at, want);
-      copy16(stage + ((TOKENS + row) * CHUNKS + (chunk ^ sv(row))) * 16, static_cast<const T*>(a.values) + at, want);
+      const uint32_t k_at = stage + (row * CHUNKS + (chunk ^ sk(row))) * 16, v_at = stage + ((TOKENS + row) * CHUNKS + (chunk ^ sv(row))) * 16;
+      if (CHUNKS > DP / PER && chunk >= DP / PER) continue;
+      if (whole) {
+        copy16(k_at, keys + (from + chunk));
+        copy16(v_at, values + (from + chunk));
+      } else {
+        const bool want = (have >> row & 1) && chunk * PER < a.D;
+        const uint32_t at = want ? from + chunk : 0;
+        copy16(k_at, keys + at, want);
+        copy16(v_at, values + at, want);
+      }
     }
   }
   return have;
@@ -339,15 +437,17 @@ __device__ __forceinline__ uint32_t transpose_matrix(uint32_t v) {
   return r;
 }
 
-template <int DP, int NT>
+template <int DP, int NT, int WAYS>
 struct HalfShape {
-  static constexpr int kTokens = 16, kTile = kWarps * kTokens, kRows = 8 * NT, kPitch = DP + 4;
-  static constexpr int kStageBytes = 2 * kTokens * DP * 2;
+  static constexpr int kMats = DP == 64 ? 2 : 1;               // 16-token matrices of a warp's tile
+  static constexpr int kTokens = 16 * kMats, kTile = kWarps / WAYS * kTokens, kRows = 8 * NT, kWays = WAYS;
+  static constexpr int kChunks = DP == 96 ? 16 : DP / 8, kRowBytes = kChunks * 16;      // (a power of two, for the swizzle)
+  static constexpr int kStageBytes = 2 * kTokens * kRowBytes;
   // stages and resident blocks per SM: as many as 227 KB hold
-  static constexpr int kStages = DP == 64 ? 4 : NT == 2 ? 2 : 3;
-  static constexpr int kResident = DP == 256 ? 1 : DP == 64 && NT == 1 ? 3 : 2;
-  static constexpr int kSumBytes = kWarps * kRows * kPitch * 4;
-  static constexpr int kShared = kWarps * kStages * kStageBytes + kSumBytes;
+  static constexpr int kStages = DP == 96 ? 2 : 3;
+  static constexpr int kResident = DP == 256 ? 1 : DP == 96 ? 3 : 2;
+  static constexpr int kShared = kWarps * kStages * kStageBytes;
+  static_assert(WAYS > 1 || kRows * DP * 4 <= kStageBytes, "a warp's sums go through a stage");
 };
 
 // Scores as keys x queries (16 tokens x 8 heads, products of 16-bit values exact, sums in 32 bits), weighted values as
@@ -356,21 +456,21 @@ struct HalfShape {
 // go from one shape to the other by transposing 8 x 8 matrices, as two 16-bit parts each (value and remainder), which
 // holds them to 2^-17 (bf16) or 2^-22 (fp16): one part alone would cost up to 2^-9 of sum w |v|, more than the rounding
 // of the result where values cancel, and the second product is hidden behind the loads.
-template <class T, int DP, int NT>
-__global__ void __launch_bounds__(kThreads) k_attention_half(AttentionArgs a) {
+template <class T, int DP, int NT, int WAYS>
+__global__ void __launch_bounds__(kThreads, HalfShape<DP, NT, WAYS>::kResident) k_attention_half(AttentionArgs a) {
   using H = Half<T>;
-  using S = HalfShape<DP, NT>;
+  using S = HalfShape<DP, NT, WAYS>;
+  constexpr int MT = S::kMats;
   extern __shared__ __align__(128) unsigned char shared[];
   __shared__ long long scan[kWarps];
   __shared__ Place place;
   __shared__ float ml[2 * kWarps * S::kRows];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   if (a.parts) cudaTriggerProgrammaticLaunchCompletion();
-  float* sums = reinterpret_cast<float*>(shared + kWarps * S::kStages * S::kStageBytes);
   Cursor<S::kTile> c = find_place<T, S::kTile>(a, &place, scan);
-  int4 join = make_int4(-1, 0, 0, 0);
+  int4 join = make_int4(-1, 0, 0, 0);          // (by block)
   if (c.left <= 0) {
-    if (a.parts && threadIdx.x == 0) a.joins[blockIdx.x] = join;
+    if (a.parts && !a.by_unit && threadIdx.x == 0) a.joins[blockIdx.x] = join;
     return;
   }
   const uint32_t ring = shared_address(shared) + warp * S::kStages * S::kStageBytes;
@@ -379,16 +479,19 @@ __global__ void __launch_bounds__(kThreads) k_attention_half(AttentionArgs a) {
   const int k_row = (lane & 7) + (lane >> 3 & 1) * 8, k_half = lane >> 4;
   const int v_row = (lane & 7) + (lane >> 4) * 8, v_half = lane >> 3 & 1;
 
+  const int per = a.units / (a.Hk / WAYS);     // units of WAYS key heads
+  const auto kv_of = [&](int unit) { return (per == 1 ? unit : unit / per) * WAYS + (WAYS > 1 ? warp : 0); };
+  const int first = WAYS > 1 ? 0 : warp * S::kTokens;
   Cursor<S::kTile> next = c;
-  Ahead ahead = look_ahead<S::kTile, S::kTokens>(a, next, warp, lane);
+  Ahead ahead = look_ahead<S::kTile, S::kTokens>(a, next, first, lane);
   uint32_t have[S::kStages];
 #pragma unroll
   for (int s = 0; s < S::kStages - 1; ++s) {
     have[s] = 0;
     if (next.left > 0) {
-      have[s] = ask_for<T, DP, S::kTokens>(a, next, ahead, ring + s * S::kStageBytes, lane, swizzle, swizzle);
+      have[s] = ask_for<T, DP, S::kChunks, S::kTokens>(a, next, ahead, ring + s * S::kStageBytes, lane, kv_of(next.unit), swizzle, swizzle);
       next.advance(a);
-      ahead = look_ahead<S::kTile, S::kTokens>(a, next, warp, lane);
+      ahead = look_ahead<S::kTile, S::kTokens>(a, next, first, lane);
     }
     commit_copies();
   }
@@ -399,7 +502,7 @@ __global__ void __launch_bounds__(kThreads) k_attention_half(AttentionArgs a) {
   while (c.left > 0) {
     if (fresh) {                               // a unit's queries: column n of B is head n, its rows are dimensions
       fresh = false;
-      const int per = a.units / a.Hk, head0 = c.unit % per * S::kRows, kv = c.unit / per;
+      const int head0 = c.unit % per * S::kRows, kv = kv_of(c.unit);
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
         const int head = head0 + n * 8 + (lane >> 2);
@@ -421,9 +524,9 @@ __global__ void __launch_bounds__(kThreads) k_attention_half(AttentionArgs a) {
       int to = stage + S::kStages - 1;
       if (to >= S::kStages) to -= S::kStages;
       if (next.left > 0) {
-        got = ask_for<T, DP, S::kTokens>(a, next, ahead, ring + to * S::kStageBytes, lane, swizzle, swizzle);
+        got = ask_for<T, DP, S::kChunks, S::kTokens>(a, next, ahead, ring + to * S::kStageBytes, lane, kv_of(next.unit), swizzle, swizzle);
         next.advance(a);
-        ahead = look_ahead<S::kTile, S::kTokens>(a, next, warp, lane);
+        ahead = look_ahead<S::kTile, S::kTokens>(a, next, first, lane);
       }
       commit_copies();
     }
@@ -434,60 +537,79 @@ __global__ void __launch_bounds__(kThreads) k_attention_half(AttentionArgs a) {
     for (int s = 0; s + 1 < S::kStages - 1; ++s) have[s] = have[s + 1];
     have[S::kStages - 2] = got;
     if (valid) {
-      const uint32_t keys = ring + stage * S::kStageBytes, values = keys + S::kTokens * DP * 2;
-      float s[NT][4];
+      const uint32_t keys = ring + stage * S::kStageBytes, values = keys + S::kTokens * S::kRowBytes;
+      // two sums each, over the even and the odd steps: half the chain of dependent instructions
+      float s[MT][NT][4], odd[MT][NT][4];
 #pragma unroll
-      for (int n = 0; n < NT; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0;
+      for (int t = 0; t < MT; ++t)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s[t][n][i] = odd[t][n][i] = 0;
 #pragma unroll
       for (int k = 0; k < DP / 16; ++k) {
-        uint32_t f[4];
-        load_matrices(f, keys + k_row * DP * 2 + (((k * 2 + k_half) ^ (k_row & 7)) << 4));
 #pragma unroll
-        for (int n = 0; n < NT; ++n) H::mma(s[n], f, q[n][k][0], q[n][k][1]);
+        for (int t = 0; t < MT; ++t) {
+          uint32_t f[4];
+          load_matrices(f, keys + (t * 16 + k_row) * S::kRowBytes + (((k * 2 + k_half) ^ (k_row & 7)) << 4));
+#pragma unroll
+          for (int n = 0; n < NT; ++n) H::mma(k & 1 ? odd[t][n] : s[t][n], f, q[n][k][0], q[n][k][1]);
+        }
       }
-      const bool low = valid >> (lane >> 2) & 1, high = valid >> ((lane >> 2) + 8) & 1;
-      uint32_t w_hi[NT][2], w_lo[NT][2];
+      uint32_t w_hi[MT][NT][2], w_lo[MT][NT][2];
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
+        float top[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s[n][i] = (i < 2 ? low : high) ? s[n][i] * a.scale_log2 : -INFINITY;
-        float top[2];
+        for (int t = 0; t < MT; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const bool is = valid >> (t * 16 + (lane >> 2) + (i & 2) * 4) & 1;
+            const float x = (s[t][n][i] + odd[t][n][i]) * a.scale_log2;
+            s[t][n][i] = is ? x : -INFINITY;
+            top[i & 1] = fmaxf(top[i & 1], is ? fmaxf(x, -FLT_MAX) : -INFINITY);
+          }
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          top[i] = fmaxf(low ? fmaxf(s[n][i], -FLT_MAX) : -INFINITY, high ? fmaxf(s[n][i + 2], -FLT_MAX) : -INFINITY);
 #pragma unroll
           for (int d = 4; d < 32; d <<= 1) top[i] = fmaxf(top[i], __shfl_xor_sync(~0u, top[i], d));
           top[i] = fmaxf(top[i], m[n][i]);
         }
         if (__any_sync(~0u, top[0] > m[n][0] || top[1] > m[n][1])) {
-          const float f0 = exp2f(m[n][0] - top[0]), f1 = exp2f(m[n][1] - top[1]);     // (valid: the new maxima are finite, or above)
+          const float f0 = power2(m[n][0] - top[0]), f1 = power2(m[n][1] - top[1]);     // (valid: the new maxima are finite, or above)
 #pragma unroll
           for (int k = 0; k < DP / 16; ++k) o[n][k][0] *= f0, o[n][k][1] *= f1, o[n][k][2] *= f0, o[n][k][3] *= f1;
           l[n][0] *= f0, l[n][1] *= f1;
           m[n][0] = top[0], m[n][1] = top[1];
         }
-        float w[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = exp2f(s[n][i] - m[n][i & 1] + H::kRaise);
-        l[n][0] += w[0] + w[2];
-        l[n][1] += w[1] + w[3];
+        for (int t = 0; t < MT; ++t) {
+          float w[4];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const uint32_t hi = H::pack(w[2 * i], w[2 * i + 1]);
-          const float2 back = H::unpack(hi);
-          const uint32_t lo = H::pack(w[2 * i] - back.x, w[2 * i + 1] - back.y);
-          w_hi[n][i] = transpose_matrix(hi);
-          w_lo[n][i] = transpose_matrix(lo);
+          for (int i = 0; i < 4; ++i) w[i] = power2(s[t][n][i] - m[n][i & 1] + H::kRaise);
+          l[n][0] += w[0] + w[2];
+          l[n][1] += w[1] + w[3];
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const uint32_t hi = H::pack(w[2 * i], w[2 * i + 1]);
+            const float2 back = H::unpack(hi);
+            const uint32_t lo = H::pack(w[2 * i] - back.x, w[2 * i + 1] - back.y);
+            w_hi[t][n][i] = transpose_matrix(hi);
+            w_lo[t][n][i] = transpose_matrix(lo);
+          }
         }
       }
 #pragma unroll
       for (int k = 0; k < DP / 16; ++k) {
-        uint32_t f[4];
-        load_matrices_transposed(f, values + v_row * DP * 2 + (((k * 2 + v_half) ^ (v_row & 7)) << 4));
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          H::mma(o[n][k], f, w_hi[n][0], w_hi[n][1]);
-          H::mma(o[n][k], f, w_lo[n][0], w_lo[n][1]);
+        for (int t = 0; t < MT; ++t) {
+          uint32_t f[4];
+          load_matrices_transposed(f, values + (t * 16 + v_row) * S::kRowBytes + (((k * 2 + v_half) ^ (v_row & 7)) << 4));
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            H::mma(o[n][k], f, w_hi[t][n][0], w_hi[t][n][1]);
+            H::mma(o[n][k], f, w_lo[t][n][0], w_lo[t][n][1]);
+          }
         }
       }
     }
@@ -495,47 +617,86 @@ __global__ void __launch_bounds__(kThreads) k_attention_half(AttentionArgs a) {
     if (++stage == S::kStages) stage = 0;
     const bool to_end = c.tile + 1 == c.tiles;
     if (to_end || c.left == 1) {
+      const int head0 = c.unit % per * S::kRows, kv = kv_of(c.unit);
+      const bool whole = from_start && to_end;
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < 2; ++i)
 #pragma unroll
           for (int d = 4; d < 32; d <<= 1) l[n][i] += __shfl_xor_sync(~0u, l[n][i], d);
-          const int row = n * 8 + (lane & 3) * 2 + i;
-          if (lane < 4) {
-            ml[warp * S::kRows + row] = m[n][i];
-            ml[(kWarps + warp) * S::kRows + row] = l[n][i];
-          }
-          float* to = sums + (size_t)(warp * S::kRows + row) * S::kPitch + (lane >> 2);
+      }
+      if constexpr (WAYS > 1) {                // a warp has the unit's tokens for its own key head
+        const Records<DP, S::kRows * WAYS> to(a);
 #pragma unroll
-          for (int k = 0; k < DP / 16; ++k) to[k * 16] = o[n][k][i], to[k * 16 + 8] = o[n][k][i + 2];
-        }
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const int row = n * 8 + (lane & 3) * 2 + i;
+            if (head0 + row >= a.group) continue;
+            if (whole) {
+              T* out = static_cast<T*>(a.out) + ((size_t)c.b * a.Hq + (size_t)kv * a.group + head0 + row) * a.D + (lane >> 2);
+              const bool none = m[n][i] == -INFINITY;
+#pragma unroll
+              for (int k = 0; k < DP / 16; ++k) {
+                if (k * 16 < a.D) out[k * 16] = narrow<T>(none ? 0.0f : __fdiv_rn(o[n][k][i], l[n][i]));
+                if (k * 16 + 8 < a.D) out[k * 16 + 8] = narrow<T>(none ? 0.0f : __fdiv_rn(o[n][k][i + 2], l[n][i]));
+              }
+            } else {
+              const size_t at = to.row(blockIdx.x, from_start, warp * S::kRows + row);
+              float* sum = to.sums + at * DP + (lane >> 2);
+#pragma unroll
+              for (int k = 0; k < DP / 16; ++k) sum[k * 16] = o[n][k][i], sum[k * 16 + 8] = o[n][k][i + 2];
+              if (lane < 4) to.tops[at] = m[n][i], to.weights[at] = l[n][i];
+            }
+          }
+      } else {                                 // through the stage just read, which is filled again only behind this
+        const int used = (stage == 0 ? S::kStages : stage) - 1;
+        float* sums = reinterpret_cast<float*>(shared + used * S::kStageBytes);
+        constexpr int kStride = S::kStages * S::kStageBytes / 4;
+        __syncwarp();
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const int row = n * 8 + (lane & 3) * 2 + i;
+            if (lane < 4) {
+              ml[warp * S::kRows + row] = m[n][i];
+              ml[(kWarps + warp) * S::kRows + row] = l[n][i];
+            }
+            float* to = sums + warp * kStride + row * DP;
+#pragma unroll
+            for (int k = 0; k < DP / 16; ++k) {
+              to[(k * 16 + (lane >> 2)) ^ spread(row)] = o[n][k][i];
+              to[(k * 16 + 8 + (lane >> 2)) ^ spread(row)] = o[n][k][i + 2];
+            }
+          }
+        __syncthreads();
+        finish_unit<T, DP, S::kRows, true>(a, c.b, kv, head0, from_start, to_end, sums, kStride, ml);
+        __syncthreads();
       }
-      __syncthreads();
-      finish_unit<T, DP, S::kRows, S::kPitch, S::kTile>(a, c, from_start, to_end, sums, ml);
-      if (from_start && !to_end) {
-        const long long unit_end = run_start(blockIdx.x + 1, place.total, place.blocks) - 1 - c.tile + c.tiles;   // in tiles of the list
-        join = make_int4(c.b, c.unit, (int)((unit_end * place.blocks - 1) / place.total), 0);
+      if (a.parts && from_start) {
+        const int4 of = to_end ? make_int4(-1, 0, 0, 0) : join_of(a, c, place);
+        if (!to_end) join = of;
+        if (a.by_unit && threadIdx.x == 0) a.joins[(size_t)c.b * a.units + c.unit] = of;
       }
-      __syncthreads();
       fresh = from_start = true;
     }
     c.advance(a);
   }
   wait_copies<0>();
-  if (a.parts && threadIdx.x == 0) a.joins[blockIdx.x] = join;
+  if (a.parts && !a.by_unit && threadIdx.x == 0) a.joins[blockIdx.x] = join;
 }
 
 // ---- fp32 --------------------------------------------------------------------------------------------------------------
 
 template <int DP>
 struct FloatShape {
-  static constexpr int kTokens = 8, kTile = kWarps * kTokens, kRows = 8, kPitch = DP;
+  static constexpr int kTokens = 8, kTile = kWarps * kTokens, kRows = 8, kWays = 1;
   static constexpr int kStageBytes = 2 * kTokens * DP * 4;
   static constexpr int kStages = DP == 64 ? 3 : 2;
   static constexpr int kResident = DP == 256 ? 1 : DP == 128 ? 2 : 3;
-  static constexpr int kSumBytes = kWarps * kRows * kPitch * 4, kQueryBytes = kRows * DP * 4;
-  static constexpr int kShared = kWarps * kStages * kStageBytes + kSumBytes + kQueryBytes;
+  static constexpr int kShared = kWarps * kStages * kStageBytes + kRows * DP * 4;        // (the queries behind the stages)
 };
 
 // The same walk with 32-bit multiplications and additions, eight heads at a time.  Scores: lane 4 t + p has every fourth
@@ -552,12 +713,11 @@ __global__ void __launch_bounds__(kThreads) k_attention_float(AttentionArgs a) {
   __shared__ __align__(16) float weights[kWarps][8][8], falls[kWarps][8];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   if (a.parts) cudaTriggerProgrammaticLaunchCompletion();
-  float* sums = reinterpret_cast<float*>(shared + kWarps * S::kStages * S::kStageBytes);
-  float* query = sums + kWarps * S::kRows * S::kPitch;
+  float* query = reinterpret_cast<float*>(shared + kWarps * S::kStages * S::kStageBytes);
   Cursor<S::kTile> c = find_place<float, S::kTile>(a, &place, scan);
-  int4 join = make_int4(-1, 0, 0, 0);
+  int4 join = make_int4(-1, 0, 0, 0);          // (by block)
   if (c.left <= 0) {
-    if (a.parts && threadIdx.x == 0) a.joins[blockIdx.x] = join;
+    if (a.parts && !a.by_unit && threadIdx.x == 0) a.joins[blockIdx.x] = join;
     return;
   }
   const unsigned char* ring = shared + warp * S::kStages * S::kStageBytes;
@@ -569,15 +729,15 @@ __global__ void __launch_bounds__(kThreads) k_attention_float(AttentionArgs a) {
   const int chunk = lane % (CHUNKS < 32 ? CHUNKS : 32), half = lane / (CHUNKS < 32 ? CHUNKS : 32);
 
   Cursor<S::kTile> next = c;
-  Ahead ahead = look_ahead<S::kTile, S::kTokens>(a, next, warp, lane);
+  Ahead ahead = look_ahead<S::kTile, S::kTokens>(a, next, warp * S::kTokens, lane);
   uint32_t have[S::kStages];
 #pragma unroll
   for (int s = 0; s < S::kStages - 1; ++s) {
     have[s] = 0;
     if (next.left > 0) {
-      have[s] = ask_for<float, DP, S::kTokens>(a, next, ahead, ring_at + s * S::kStageBytes, lane, swizzle_keys, plain);
+      have[s] = ask_for<float, DP, CHUNKS, S::kTokens>(a, next, ahead, ring_at + s * S::kStageBytes, lane, next.unit / (a.units / a.Hk), swizzle_keys, plain);
       next.advance(a);
-      ahead = look_ahead<S::kTile, S::kTokens>(a, next, warp, lane);
+      ahead = look_ahead<S::kTile, S::kTokens>(a, next, warp * S::kTokens, lane);
     }
     commit_copies();
   }
@@ -605,9 +765,9 @@ __global__ void __launch_bounds__(kThreads) k_attention_float(AttentionArgs a) {
       int to = stage + S::kStages - 1;
       if (to >= S::kStages) to -= S::kStages;
       if (next.left > 0) {
-        got = ask_for<float, DP, S::kTokens>(a, next, ahead, ring_at + to * S::kStageBytes, lane, swizzle_keys, plain);
+        got = ask_for<float, DP, CHUNKS, S::kTokens>(a, next, ahead, ring_at + to * S::kStageBytes, lane, next.unit / (a.units / a.Hk), swizzle_keys, plain);
         next.advance(a);
-        ahead = look_ahead<S::kTile, S::kTokens>(a, next, warp, lane);
+        ahead = look_ahead<S::kTile, S::kTokens>(a, next, warp * S::kTokens, lane);
       }
       commit_copies();
     }
@@ -658,8 +818,8 @@ __global__ void __launch_bounds__(kThreads) k_attention_float(AttentionArgs a) {
       rises = __any_sync(~0u, rises);
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const float fall = exp2f(m[i] - top[i]);
-        const float w = exp2f(t2[i] - top[i]);
+        const float fall = power2(m[i] - top[i]);
+        const float w = power2(t2[i] - top[i]);
         l[i] = fmaf(l[i], fall, w);
         m[i] = top[i];
         weights[warp][head + i][token] = w;
@@ -700,6 +860,9 @@ __global__ void __launch_bounds__(kThreads) k_attention_float(AttentionArgs a) {
     if (++stage == S::kStages) stage = 0;
     const bool to_end = c.tile + 1 == c.tiles;
     if (to_end || c.left == 1) {
+      const int per = a.units / a.Hk, used = (stage == 0 ? S::kStages : stage) - 1;
+      float* sums = reinterpret_cast<float*>(shared + used * S::kStageBytes);      // through the stage just read
+      constexpr int kStride = S::kStages * S::kStageBytes / 4;
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
 #pragma unroll
@@ -717,13 +880,14 @@ __global__ void __launch_bounds__(kThreads) k_attention_float(AttentionArgs a) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) o[h][v][i] += __shfl_xor_sync(~0u, o[h][v][i], 16);
           if (half == 0)
-            *reinterpret_cast<float4*>(sums + (size_t)(warp * S::kRows + h) * S::kPitch + (chunk + v * 32) * 4) = make_float4(o[h][v][0], o[h][v][1], o[h][v][2], o[h][v][3]);
+            *reinterpret_cast<float4*>(sums + warp * kStride + h * DP + (chunk + v * 32) * 4) = make_float4(o[h][v][0], o[h][v][1], o[h][v][2], o[h][v][3]);
         }
       __syncthreads();
-      finish_unit<float, DP, S::kRows, S::kPitch, S::kTile>(a, c, from_start, to_end, sums, ml);
-      if (from_start && !to_end) {
-        const long long unit_end = run_start(blockIdx.x + 1, place.total, place.blocks) - 1 - c.tile + c.tiles;
-        join = make_int4(c.b, c.unit, (int)((unit_end * place.blocks - 1) / place.total), 0);
+      finish_unit<float, DP, S::kRows, false>(a, c.b, c.unit / per, c.unit % per * S::kRows, from_start, to_end, sums, kStride, ml);
+      if (a.parts && from_start) {
+        const int4 of = to_end ? make_int4(-1, 0, 0, 0) : join_of(a, c, place);
+        if (!to_end) join = of;
+        if (a.by_unit && threadIdx.x == 0) a.joins[(size_t)c.b * a.units + c.unit] = of;
       }
       __syncthreads();
       fresh = from_start = true;
@@ -731,7 +895,7 @@ __global__ void __launch_bounds__(kThreads) k_attention_float(AttentionArgs a) {
     c.advance(a);
   }
   wait_copies<0>();
-  if (a.parts && threadIdx.x == 0) a.joins[blockIdx.x] = join;
+  if (a.parts && !a.by_unit && threadIdx.x == 0) a.joins[blockIdx.x] = join;
 }
 
 // ---- launches ------------------------------------------------------------------------------------------------------------
@@ -742,24 +906,27 @@ AttentionArgs arguments(const ClusterLaunch& L) {
   const bool empty = slot(L, 1).R == 0;                       // (a copy of no bytes still names an address)
   return {report_of(L), slot(L, 0).ptr, slot(L, empty ? 0 : 1).ptr, slot(L, empty ? 0 : 2).ptr, slot_ptr<int>(L, 3), slot_ptr<int>(L, 4), result_ptr<void>(L),
           (int)L.op.shape[0], slot(L, 3).C, slot(L, 1).R, Hq, Hk, D, (int)std::min<int64_t>(L.op.iparam[2], 0x7FFFFFFF),
-          Hk > 0 ? Hq / Hk : 0, 0, (float)(L.op.fparam[0] * 1.4426950408889634), divisor((uint32_t)L.op.iparam[0]), nullptr, nullptr};
+          Hk > 0 ? Hq / Hk : 0, 0, (float)(L.op.fparam[0] * 1.4426950408889634), divisor((uint32_t)L.op.iparam[0]), nullptr, 0, 0, nullptr, false};
 }
 
 // Blocks of the grid, and whether a unit may be split: never if no request can have more than a tile.
 template <class S>
 int grid_of(AttentionArgs& a, bool& splits) {
-  a.units = a.Hk * ((a.group + S::kRows - 1) / S::kRows);
+  a.units = a.Hk / S::kWays * ((a.group + S::kRows - 1) / S::kRows);
   const long long room = (long long)a.W * a.block.d;
   const long long tiles = std::max<long long>((room + S::kTile - 1) / S::kTile, 1) * a.B * a.units;
   splits = room > S::kTile;
-  return (int)std::min<long long>(tiles, (long long)sm_count() * S::kResident);
+  return a.grid = (int)std::min<long long>(tiles, std::min((long long)sm_count() * S::kResident, (long long)kMaxGrid));
 }
+
+// Entries of AttentionArgs::joins.
+long long joins_of(const AttentionArgs& a) { return std::min<long long>(a.grid, (long long)a.B * a.units); }
 
 template <class S, int DP>
 int64_t scratch_of(AttentionArgs a) {
   bool splits;
   const int64_t grid = grid_of<S>(a, splits);
-  return splits ? grid * (16 + 2 * S::kRows * (DP + 2) * 4) : 0;
+  return splits ? joins_of(a) * 16 + (int64_t)Records<DP, S::kRows * S::kWays>::bytes((int)grid) : 0;
 }
 
 template <class T, int DP, class S, class K>
@@ -769,7 +936,8 @@ int run(const ClusterLaunch& L, K kernel, std::atomic<uint64_t>& allowed) {
   const int grid = grid_of<S>(a, splits);
   if (splits) {
     a.joins = reinterpret_cast<int4*>(L.scratch);
-    a.parts = reinterpret_cast<float*>(a.joins + grid);
+    a.by_unit = (long long)a.B * a.units <= grid;
+    a.parts = reinterpret_cast<float*>(a.joins + joins_of(a));
   }
   const int rc = allow_shared(kernel, S::kShared, allowed);
   if (rc != ACC_OK) return rc;
@@ -777,8 +945,10 @@ int run(const ClusterLaunch& L, K kernel, std::atomic<uint64_t>& allowed) {
   if (!splits) return launched();
   // the joining kernel is launched early and waits for the first one on the device
   cudaLaunchConfig_t config{};
-  config.gridDim = dim3(grid, std::min(S::kRows, a.group));
-  config.blockDim = dim3(256);
+  const int heads = S::kRows * S::kWays;
+  a.join_rows = (long long)a.B * a.units * kManyRecords < grid ? 1 : 8;
+  config.gridDim = dim3((unsigned)joins_of(a), heads / a.join_rows, a.join_rows == 1 ? DP / kPiece : 1);
+  config.blockDim = dim3(kJoinThreads);
   config.stream = L.stream;
   cudaLaunchAttribute early{};
   early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -786,32 +956,40 @@ int run(const ClusterLaunch& L, K kernel, std::atomic<uint64_t>& allowed) {
   config.attrs = &early;
   config.numAttrs = 1;
   ++L.extra_launches;
-  const cudaError_t e = cudaLaunchKernelEx(&config, k_join<T, DP, S::kRows>, a);
+  const cudaError_t e = cudaLaunchKernelEx(&config, k_join<T, DP, S::kRows, S::kWays>, a);
   return e == cudaSuccess ? launched() : set_error(ACC_ERR_CUDA, "kernel launch failed: %s", cudaGetErrorString(cudaGetLastError()));
 }
 
-// Calls f(shape, DP, pointer to the kernel, flags) for the kernel that a launch takes: heads padded to 64, 128 or 256
-// elements; for 16-bit types sixteen heads at a time where a key head has more than eight (a head of up to 128 elements:
-// beyond, the registers do not hold them).
+// Calls f(type, DP, shape, kernel) for the kernel that a launch takes: heads padded to 64, 96, 128 or 256 elements; for
+// 16-bit types sixteen heads at a time where a key head has more than eight (beyond 128 elements the registers do not hold
+// them), and the four warps on four key heads where there are so many: their rows lie side by side, so that what is read
+// together is four times as long.
+constexpr int kManyHeads = 128;
+template <class T, int DP, int NT, class F>
+auto choose_ways(const ClusterLaunch& L, F f) {
+  const std::integral_constant<int, DP> dp{};
+  const int Hk = slot(L, 1).C / (int)L.op.iparam[1];
+  if (Hk % kWarps == 0 && L.op.shape[0] * Hk >= kManyHeads) return f(T{}, dp, HalfShape<DP, NT, kWarps>{}, k_attention_half<T, DP, NT, kWarps>);
+  return f(T{}, dp, HalfShape<DP, NT, 1>{}, k_attention_half<T, DP, NT, 1>);
+}
+template <class T, class F>
+auto choose_half(const ClusterLaunch& L, F f) {
+  const int D = (int)L.op.iparam[1];
+  const bool wide = (int)L.op.shape[1] > 8 * slot(L, 1).C;
+  if (D <= 64) return wide ? choose_ways<T, 64, 2>(L, f) : choose_ways<T, 64, 1>(L, f);
+  if (D <= 96) return wide ? choose_ways<T, 96, 2>(L, f) : choose_ways<T, 96, 1>(L, f);
+  if (D <= 128) return wide ? choose_ways<T, 128, 2>(L, f) : choose_ways<T, 128, 1>(L, f);
+  return choose_ways<T, 256, 1>(L, f);
+}
 template <class F>
 auto choose(const ClusterLaunch& L, F f) {
   const int D = (int)L.op.iparam[1];
-  const int Hk = slot(L, 1).C / D, group = Hk > 0 ? (int)L.op.shape[1] / D / Hk : 0;
-  const bool wide = group > 8;
   if (L.op.dtype == ACC_F32) {
     if (D <= 64) return f(float{}, std::integral_constant<int, 64>{}, FloatShape<64>{}, k_attention_float<64>);
     if (D <= 128) return f(float{}, std::integral_constant<int, 128>{}, FloatShape<128>{}, k_attention_float<128>);
     return f(float{}, std::integral_constant<int, 256>{}, FloatShape<256>{}, k_attention_float<256>);
   }
-  const auto half = [&](auto t) {
-    using T = decltype(t);
-    if (D <= 64) return wide ? f(t, std::integral_constant<int, 64>{}, HalfShape<64, 2>{}, k_attention_half<T, 64, 2>)
-                             : f(t, std::integral_constant<int, 64>{}, HalfShape<64, 1>{}, k_attention_half<T, 64, 1>);
-    if (D <= 128) return wide ? f(t, std::integral_constant<int, 128>{}, HalfShape<128, 2>{}, k_attention_half<T, 128, 2>)
-                              : f(t, std::integral_constant<int, 128>{}, HalfShape<128, 1>{}, k_attention_half<T, 128, 1>);
-    return f(t, std::integral_constant<int, 256>{}, HalfShape<256, 1>{}, k_attention_half<T, 256, 1>);
-  };
-  return L.op.dtype == ACC_F16 ? half(__half{}) : half(__nv_bfloat16{});
+  return L.op.dtype == ACC_F16 ? choose_half<__half>(L, f) : choose_half<__nv_bfloat16>(L, f);
 }
 
 bool nothing(const ClusterLaunch& L) { return L.op.shape[0] == 0 || L.op.shape[1] == 0; }

@@ -251,7 +251,8 @@ int acc_edges(const acc_graph* g, int32_t* F, int32_t* nF, int32_t* I, int32_t* 
  *                           x = x - frequency * c;  x = x - presence if c > 0
  *       v among bias_ids[b]: x = x + the sum of its biases, added up in list order
  *       M > 0 and bit v mod 32 of mask[b, v / 32] not set: x = -infinity
- *     Negative tokens and ids are padding.  M is 0 (no mask) or ceil(V / 32).
+ *     Negative tokens and ids are padding.  M is 0 (no mask) or ceil(V / 32), K is
+ *     at most 65535.
  *     Logits and result have one element type of F32, F16, BF16.  May be bound in
  *     place of the logits.  Reported: a token or id beyond V (left out).
  *

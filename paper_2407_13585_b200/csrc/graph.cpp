@@ -124,6 +124,7 @@ static int check_operator(const Graph& g, const acc_node_desc& d, int id) {
       const int64_t B = d.shape[0], words = (d.shape[1] + 31) / 32;
       if (in(1).rank != 2 || in(1).shape[0] != B || !is_shape(in(2), B, 4) || in(3).rank != 2 || in(3).shape[0] != B || !same_shape(in(3), in(4)))
         return set_error(ACC_ERR_SHAPE, "node %d: tokens, 4 parameters, ids and biases for every row", id);
+      if (in(3).shape[1] > 65535) return set_error(ACC_ERR_UNSUPPORTED, "node %d: more than 65535 biases a row", id);
       if (!is_shape(in(5), B, 0) && !is_shape(in(5), B, words)) return set_error(ACC_ERR_SHAPE, "node %d: the mask has 0 or %lld words a row", id, (long long)words);
       return ACC_OK;
     }

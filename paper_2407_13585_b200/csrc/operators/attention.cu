@@ -229,7 +229,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_join(AttentionArgs a) {
   __shared__ float weight[kMaxGrid];
   __shared__ float tops[kJoinWarps], shares[kJoinWarps];
   __shared__ float4 sums[kJoinWarps][kPiece / 4];
-  cudaGridDependencySynchronize();
+  follow();
   const int4 join = a.joins[blockIdx.x];
   if (join.x < 0) return;
   const int per = a.units / (a.Hk / WAYS), head0 = join.y % per * ROWS;
@@ -466,7 +466,7 @@ __global__ void __launch_bounds__(kThreads, HalfShape<DP, NT, WAYS>::kResident) 
   __shared__ Place place;
   __shared__ float ml[2 * kWarps * S::kRows];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  if (a.parts) cudaTriggerProgrammaticLaunchCompletion();
+  cudaTriggerProgrammaticLaunchCompletion();
   Cursor<S::kTile> c = find_place<T, S::kTile>(a, &place, scan);
   int4 join = make_int4(-1, 0, 0, 0);          // (by block)
   if (c.left <= 0) {
@@ -712,7 +712,7 @@ __global__ void __launch_bounds__(kThreads) k_attention_float(AttentionArgs a) {
   __shared__ float ml[2 * kWarps * S::kRows];
   __shared__ __align__(16) float weights[kWarps][8][8], falls[kWarps][8];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  if (a.parts) cudaTriggerProgrammaticLaunchCompletion();
+  cudaTriggerProgrammaticLaunchCompletion();
   float* query = reinterpret_cast<float*>(shared + kWarps * S::kStages * S::kStageBytes);
   Cursor<S::kTile> c = find_place<float, S::kTile>(a, &place, scan);
   int4 join = make_int4(-1, 0, 0, 0);          // (by block)
@@ -941,23 +941,15 @@ int run(const ClusterLaunch& L, K kernel, std::atomic<uint64_t>& allowed) {
   }
   const int rc = allow_shared(kernel, S::kShared, allowed);
   if (rc != ACC_OK) return rc;
-  kernel<<<grid, kThreads, S::kShared, L.stream>>>(a);
-  if (!splits) return launched();
-  // the joining kernel is launched early and waits for the first one on the device
-  cudaLaunchConfig_t config{};
-  const int heads = S::kRows * S::kWays;
   a.join_rows = (long long)a.B * a.units * kManyRecords < grid ? 1 : 8;
-  config.gridDim = dim3((unsigned)joins_of(a), heads / a.join_rows, a.join_rows == 1 ? DP / kPiece : 1);
-  config.blockDim = dim3(kJoinThreads);
-  config.stream = L.stream;
-  cudaLaunchAttribute early{};
-  early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  early.val.programmaticStreamSerializationAllowed = 1;
-  config.attrs = &early;
-  config.numAttrs = 1;
+  // (not launched early: beside the kernel before it an SM is divided for less shared memory, and keeps to that while the
+  // blocks that did fit run; 31 windows of 4096 tokens, back to back: 101 us, launched early 154)
+  kernel<<<grid, kThreads, S::kShared, L.stream>>>(a);
+  const int first = launched();
+  if (first != ACC_OK || !splits) return first;
   ++L.extra_launches;
-  const cudaError_t e = cudaLaunchKernelEx(&config, k_join<T, DP, S::kRows, S::kWays>, a);
-  return e == cudaSuccess ? launched() : set_error(ACC_ERR_CUDA, "kernel launch failed: %s", cudaGetErrorString(cudaGetLastError()));
+  return launch_following(k_join<T, DP, S::kRows, S::kWays>, dim3((unsigned)joins_of(a), S::kRows * S::kWays / a.join_rows, a.join_rows == 1 ? DP / kPiece : 1),
+                          kJoinThreads, 0, L.stream, a);
 }
 
 // Calls f(type, DP, shape, kernel) for the kernel that a launch takes: heads padded to 64, 96, 128 or 256 elements; for

@@ -48,6 +48,29 @@ __device__ __forceinline__ uint32_t operator/(uint32_t v, const Divisor& p) {
 // The blocks that `length` tokens take up.
 __device__ __forceinline__ int blocks_of(int length, const Divisor& block) { return length <= 0 ? 0 : (int)((uint32_t)(length - 1) / block) + 1; }
 
+// Launches a kernel so that it may be set up while the one before it in the stream still runs.  It begins with
+// follow(): nothing is read or written before everything that was launched earlier has finished and its results are
+// visible.  (A kernel that begins so may follow another one: each of them ends only after it has waited.)
+template <class... P, class... A>
+int launch_following(void (*kernel)(P...), dim3 grid, int threads, size_t shared, cudaStream_t stream, const A&... args) {
+  cudaLaunchConfig_t config{};
+  config.gridDim = grid;
+  config.blockDim = dim3(threads);
+  config.dynamicSmemBytes = shared;
+  config.stream = stream;
+  cudaLaunchAttribute early{};
+  early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  early.val.programmaticStreamSerializationAllowed = 1;
+  config.attrs = &early;
+  config.numAttrs = 1;
+  const cudaError_t e = cudaLaunchKernelEx(&config, kernel, args...);
+  return e == cudaSuccess ? ACC_OK : set_error(ACC_ERR_CUDA, "kernel launch failed: %s", cudaGetErrorString((cudaGetLastError(), e)));
+}
+__device__ __forceinline__ void follow() {
+  cudaTriggerProgrammaticLaunchCompletion();
+  cudaGridDependencySynchronize();
+}
+
 inline int launched() {
   const cudaError_t e = cudaGetLastError();
   return e == cudaSuccess ? ACC_OK : set_error(ACC_ERR_CUDA, "kernel launch failed: %s", cudaGetErrorString(e));

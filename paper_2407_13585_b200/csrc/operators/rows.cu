@@ -31,14 +31,17 @@ constexpr int kUnitsPerLane = 4;
 template <int BYTES>
 __global__ void __launch_bounds__(128) k_put_rows(RowArgs a) {
   using U = typename Unit<BYTES>::type;
+  // behind the kernels that settle owners only they are waited for, and only once the row is on its way: they were not
+  // launched before what the slots and rows come from had finished
+  if (a.owner) cudaTriggerProgrammaticLaunchCompletion();
+  else follow();
   const int lane = threadIdx.x & 31;
   const long long w = (long long)blockIdx.x * (blockDim.x / 32) + (threadIdx.x >> 5);
   const int t = (int)(w / a.pieces), piece = (int)(w % a.pieces);
-  if (t >= a.T) return;
-  const int at = a.slots[t];
-  if (at < 0) return;
-  if (at >= a.S) {
-    if (lane == 0) raise_index(a.report);
+  const int at = t < a.T ? a.slots[t] : -1;
+  if (at >= a.S && lane == 0) raise_index(a.report);
+  if (at < 0 || at >= a.S) {
+    if (a.owner) cudaGridDependencySynchronize();
     return;
   }
   const int first = piece * 32 * kUnitsPerLane + lane;
@@ -48,8 +51,10 @@ __global__ void __launch_bounds__(128) k_put_rows(RowArgs a) {
   for (int k = 0; k < kUnitsPerLane; ++k)
     if (first + 32 * k < a.units) v[k] = from[first + 32 * k];
   bool later = false;
-  if (a.owner) later = a.owner[at] != t;
-  else {
+  if (a.owner) {
+    cudaGridDependencySynchronize();
+    later = a.owner[at] != t;
+  } else {
 #pragma unroll 4
     for (int i = t + 1 + lane; i < a.T; i += 32) later = later || a.slots[i] == at;
     later = __any_sync(~0u, later);
@@ -62,15 +67,18 @@ __global__ void __launch_bounds__(128) k_put_rows(RowArgs a) {
 }
 
 __global__ void __launch_bounds__(256) k_clear_owners(const int* slots, int* owner, int T, int S) {
+  cudaTriggerProgrammaticLaunchCompletion();
   const int t = blockIdx.x * 256 + threadIdx.x;
   if (t < T && slots[t] >= 0 && slots[t] < S) owner[slots[t]] = -1;
 }
 __global__ void __launch_bounds__(256) k_last_owner(const int* slots, int* owner, int T, int S) {
+  follow();
   const int t = blockIdx.x * 256 + threadIdx.x;
   if (t < T && slots[t] >= 0 && slots[t] < S) atomicMax(owner + slots[t], t);
 }
 
 __global__ void __launch_bounds__(256) k_copy_array(const uint4* from, uint4* to, size_t vectors, size_t bytes) {
+  follow();
   const size_t stride = (size_t)gridDim.x * 256;
 #pragma unroll 4
   for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < vectors; i += stride) to[i] = from[i];
@@ -91,31 +99,31 @@ int launch_put_rows(const ClusterLaunch& L) {
   if (bytes == 0) return ACC_OK;
   const void* dest = slot(L, 0).ptr;
   void* out = result_ptr<void>(L);
-  L.extra_launches = -1;
+  int launches = 0, rc = ACC_OK;
   if (dest != out) {
     const size_t vectors = bytes / 16;
     const int grid = (int)std::min<size_t>(std::max<size_t>((vectors + 1023) / 1024, 1), (size_t)sm_count() * 8);
-    k_copy_array<<<grid, 256, 0, L.stream>>>(static_cast<const uint4*>(dest), static_cast<uint4*>(out), vectors, bytes);
-    ++L.extra_launches;
+    rc = launch_following(k_copy_array, dim3(grid), 256, 0, L.stream, static_cast<const uint4*>(dest), static_cast<uint4*>(out), vectors, bytes);
+    ++launches;
   }
   RowArgs a{report_of(L), slot_ptr<int>(L, 1), slot(L, 2).ptr, out, nullptr, (int)slot(L, 1).C, (int)L.op.shape[0], 0, 1};
-  if (a.T > 0) {
+  if (a.T > 0 && rc == ACC_OK) {
     if (a.T > kRowsThatLook) {
       a.owner = reinterpret_cast<int*>(L.scratch);
+      // (launched like any other kernel: it begins when everything before it has finished)
       k_clear_owners<<<(a.T + 255) / 256, 256, 0, L.stream>>>(a.slots, a.owner, a.T, a.S);
-      k_last_owner<<<(a.T + 255) / 256, 256, 0, L.stream>>>(a.slots, a.owner, a.T, a.S);
-      L.extra_launches += 2;
+      if ((rc = launched()) == ACC_OK) rc = launch_following(k_last_owner, dim3((a.T + 255) / 256), 256, 0, L.stream, a.slots, a.owner, a.T, a.S);
+      launches += 2;
     }
     const int unit = row_bytes % 16 == 0 ? 16 : row_bytes % 4 == 0 ? 4 : 2;
     a.units = (int)(row_bytes / unit);
     a.pieces = (a.units + 32 * kUnitsPerLane - 1) / (32 * kUnitsPerLane);
-    const unsigned grid = (unsigned)(((long long)a.T * a.pieces + 3) / 4);
-    if (unit == 16) k_put_rows<16><<<grid, 128, 0, L.stream>>>(a);
-    else if (unit == 4) k_put_rows<4><<<grid, 128, 0, L.stream>>>(a);
-    else k_put_rows<2><<<grid, 128, 0, L.stream>>>(a);
-    ++L.extra_launches;
+    const dim3 grid((unsigned)(((long long)a.T * a.pieces + 3) / 4));
+    if (rc == ACC_OK) rc = launch_following(unit == 16 ? k_put_rows<16> : unit == 4 ? k_put_rows<4> : k_put_rows<2>, grid, 128, 0, L.stream, a);
+    ++launches;
   }
-  return launched();
+  L.extra_launches = launches - 1;
+  return rc;
 }
 
 const Register put_rows(ACC_PUT_ROWS, "k_put_rows", put_rows_scratch, launch_put_rows);

@@ -11,85 +11,100 @@ struct TableArgs {
   Report report;
   const int *lens, *free, *old_lens, *old;   // old_lens, old: null if every block comes from `free`
   int* out;
-  int R, W, N;
+  int R, W, N, tile;
   Divisor block, width;
 };
 
-__device__ __forceinline__ int blocks_taken(const TableArgs& a, int r) {
-  return max(blocks_of(a.lens[r], a.block) - (a.old_lens ? blocks_of(a.old_lens[r], a.block) : 0), 0);
-}
-
-// Sum over the block, and over the threads before this one (kThreads threads; `warp_sums` of kThreads / 32 words).
-__device__ __forceinline__ long long block_scan(long long v, long long* warp_sums, long long* total) {
+// Of v: the sum over the threads before this one, and over all; of w the sum over all.  (kThreads threads.)
+struct Scan {
+  long long before, all, all_w;
+};
+__device__ __forceinline__ Scan block_scan(long long v, long long w, long long (*warp_sums)[2]) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   long long incl = v;
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
     const long long below = __shfl_up_sync(~0u, incl, d);
+    w += __shfl_xor_sync(~0u, w, d);
     if (lane >= d) incl += below;
   }
-  if (lane == 31) warp_sums[warp] = incl;
+  if (lane == 31) warp_sums[warp][0] = incl, warp_sums[warp][1] = w;
   __syncthreads();
-  long long before = 0, all = 0;
+  Scan r{incl - v, 0, 0};
 #pragma unroll
-  for (int w = 0; w < kThreads / 32; ++w) {
-    if (w < warp) before += warp_sums[w];
-    all += warp_sums[w];
+  for (int k = 0; k < kThreads / 32; ++k) {
+    if (k < warp) r.before += warp_sums[k][0];
+    r.all += warp_sums[k][0];
+    r.all_w += warp_sums[k][1];
   }
   __syncthreads();
-  *total = all;
-  return before + incl - v;
+  return r;
+}
+
+__device__ __noinline__ int table_entry(const TableArgs& a, int f, int j, int first, int kept, int need) {
+  if (j >= need) return -1;
+  if (j < kept) return a.old ? a.old[f] : -1;
+  const long long at = (long long)first + j - kept;
+  return at < a.N ? a.free[at] : -1;
 }
 
 // table[r, j] = old[r, j] | free[base_r + j - had_r] | -1 with base_r the blocks that earlier requests took.  A block
-// writes a run of kTableTile elements of the table, whatever rows they belong to, and adds up for itself what the
-// requests before its first one take: one launch and no waiting on other blocks.  Bound: writing the table.  The lengths
-// that are read over again (4 R bytes for a block, from L2) are the smaller part as long as R < kTableTile.
-constexpr int kTableTile = 2048;
+// writes a run of a.tile elements of the table, whatever rows they belong to, and adds up for itself what the requests
+// before its first one take: one launch and no waiting on other blocks.  Bound: latency for small tables, then writing the
+// table; the lengths that are read over again (4 R bytes for a block, from L2) are the smaller part as long as
+// R < a.tile.  kTableRows rows at most: where they are shorter than eight elements a block takes fewer elements.
+constexpr int kTableTile = 8192, kTableRows = 1024;
 __global__ void __launch_bounds__(kThreads) k_block_table(TableArgs a) {
-  __shared__ long long warp_sums[kThreads / 32];
-  __shared__ int first_free[kTableTile + 2], had[kTableTile + 2], has[kTableTile + 2];
-  const int f0 = blockIdx.x * kTableTile, f1 = min(f0 + kTableTile, (int)((long long)a.R * a.W));
+  __shared__ long long warp_sums[kThreads / 32][2];
+  __shared__ int first_free[kTableRows + 2], had[kTableRows + 2], has[kTableRows + 2];
+  follow();
+  const int f0 = blockIdx.x * a.tile, f1 = (int)min((long long)f0 + a.tile, (long long)a.R * a.W);
   const int r0 = (uint32_t)f0 / a.width, r1 = (uint32_t)(f1 - 1) / a.width + 1;
-  long long base = 0;
-  {
-    long long mine = 0;
+  const auto length = [&](int row) { return row < r1 ? a.lens[row] : 0; };
+  const auto old_length = [&](int row) { return row < r1 && a.old_lens ? a.old_lens[row] : 0; };
+  int len = length(r0 + threadIdx.x), old_len = old_length(r0 + threadIdx.x);
+  long long earlier = 0;
 #pragma unroll 4
-    for (int r = threadIdx.x; r < r0; r += kThreads) mine += blocks_taken(a, r);
-    block_scan(mine, warp_sums, &base);
-  }
+  for (int r = threadIdx.x; r < r0; r += kThreads) earlier += max(blocks_of(a.lens[r], a.block) - (a.old_lens ? blocks_of(a.old_lens[r], a.block) : 0), 0);
+  long long base = 0;
   for (int r = r0; r < r1; r += kThreads) {
     const int row = r + threadIdx.x;
-    const int len = row < r1 ? a.lens[row] : 0, old_len = row < r1 && a.old_lens ? a.old_lens[row] : 0;
-    const int need = blocks_of(len, a.block), kept = blocks_of(old_len, a.block);
-    long long total;
-    const long long start = base + block_scan(max(need - kept, 0), warp_sums, &total);
+    if (r > r0) len = length(row), old_len = old_length(row);
+    const int need = blocks_of(len, a.block), kept = blocks_of(old_len, a.block), taken = max(need - kept, 0);
+    const Scan s = block_scan(taken, r == r0 ? earlier : 0, warp_sums);
+    base += s.all_w;
     if (row < r1) {
+      const long long start = base + s.before;
       first_free[row - r0] = (int)min(start, (long long)a.N);
       had[row - r0] = kept;
       has[row - r0] = need;
-      if (len < 0 || old_len < 0 || need > a.W || start + max(need - kept, 0) > a.N) raise_index(a.report);
+      if (len < 0 || old_len < 0 || need > a.W || start + taken > a.N) raise_index(a.report);
     }
-    base += total;
+    base += s.all;
   }
   __syncthreads();
-  const auto entry = [&](int f, int r, int j) {
-    const int need = has[r - r0], kept = had[r - r0];
-    if (j >= need) return -1;
-    if (j < kept) return a.old ? a.old[f] : -1;
-    const long long at = (long long)first_free[r - r0] + (j - kept);
-    return at < a.N ? a.free[at] : -1;
-  };
+#pragma unroll 4
   for (int f = f0 + 4 * threadIdx.x; f < f1; f += 4 * kThreads) {
-    int r = (uint32_t)f / a.width, j = f - r * a.W;
-    int v[4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      v[k] = f + k < f1 ? entry(f + k, r, j) : 0;
-      if (++j == a.W) { j = 0; ++r; }
+    const int r = (uint32_t)f / a.width, j = f - r * a.W;
+    if (f + 4 > f1 || j + 4 > a.W) {
+      for (int k = 0, row = r - r0, at = j; k < 4 && f + k < f1; ++k) {
+        a.out[f + k] = table_entry(a, f + k, at, first_free[row], had[row], has[row]);
+        if (++at == a.W) { at = 0; ++row; }
+      }
+      continue;
     }
-    if (f + 4 <= f1) *reinterpret_cast<int4*>(a.out + f) = make_int4(v[0], v[1], v[2], v[3]);
-    else for (int k = 0; f + k < f1; ++k) a.out[f + k] = v[k];
+    // four of one row: what is kept comes in one piece
+    const int need = has[r - r0], kept = min(had[r - r0], need), from = first_free[r - r0] - had[r - r0];
+    int4 x = make_int4(-1, -1, -1, -1);
+    if (a.old && j < kept) x = *reinterpret_cast<const int4*>(a.old + f);
+    int v[4] = {x.x, x.y, x.z, x.w};
+    if (j + 4 > kept) {
+      const int end = (int)min((long long)need, (long long)a.N - from);        // where the list ends
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (j + k >= kept) v[k] = j + k < end ? a.free[from + j + k] : -1;
+    }
+    *reinterpret_cast<int4*>(a.out + f) = make_int4(v[0], v[1], v[2], v[3]);
   }
 }
 
@@ -99,10 +114,13 @@ int launch_block_table(const ClusterLaunch& L) {
   if (L.op.shape[0] == 0) return ACC_OK;
   const bool grow = L.op.n_inputs == 4;
   TableArgs a{report_of(L), slot_ptr<int>(L, 0), slot_ptr<int>(L, 1), grow ? slot_ptr<int>(L, 2) : nullptr, grow ? slot_ptr<int>(L, 3) : nullptr,
-              result_ptr<int>(L), t.R, t.C, (int)slot(L, 1).C, divisor((uint32_t)L.op.iparam[0]), divisor((uint32_t)std::max<int64_t>(L.op.shape[1], 1))};
+              result_ptr<int>(L), t.R, t.C, (int)slot(L, 1).C, 0, divisor((uint32_t)L.op.iparam[0]), divisor((uint32_t)std::max<int64_t>(L.op.shape[1], 1))};
   if (count == 0) return ACC_OK;
-  k_block_table<<<(unsigned)((count + kTableTile - 1) / kTableTile), kThreads, 0, L.stream>>>(a);
-  return launched();
+  // two blocks to an SM, if that leaves each at least four elements a thread
+  const long long even = (count + 2 * sm_count() - 1) / (2 * sm_count());
+  a.tile = (int)std::min<long long>(kTableTile, (even + 4 * kThreads - 1) / (4 * kThreads) * (4 * kThreads));
+  a.tile = (int)std::min<int64_t>(a.tile, kTableRows * (int64_t)a.W);
+  return launch_following(k_block_table, dim3((unsigned)((count + a.tile - 1) / a.tile)), kThreads, 0, L.stream, a);
 }
 
 struct SlotArgs {
@@ -127,68 +145,132 @@ __device__ __forceinline__ int requests_before(const int* off, int lo, int hi, i
   return lo;
 }
 
-// A block maps a run of kSlotTile tokens.  Its first warp finds the requests of the first and the last of them; when those
-// are few (they are, unless many are empty), their offsets and lengths are brought into shared memory, and every thread
-// finds the request of its tokens there.  Bound: latency, a chain of five dependent reads; then writing the slots.
-constexpr int kSlotTile = 4 * kThreads, kSlotRows = 1024;
+// Slot of token t, which request `lo` (of those from `first` on) holds or none; -1, and bad, where there is none.
+__device__ __forceinline__ int slot_of(const SlotArgs& a, const int* off, const int* lens, int first, int rows, int lo, int t, bool& bad) {
+  if (lo >= rows || t < off[lo]) return -1;
+  const long long p = (long long)lens[lo] - ((long long)off[lo + 1] - t);
+  int page = -1;
+  uint32_t q = 0;
+  if (p >= 0) {
+    q = (uint32_t)p / a.block;
+    if (q < (uint32_t)a.W) page = a.table[(size_t)(first + lo) * a.W + q];
+  }
+  const long long at = (long long)page * a.block.d + (p - (long long)q * a.block.d);
+  if (page < 0 || at > 0x7FFFFFFFll) {
+    bad = true;
+    return -1;
+  }
+  return (int)at;
+}
+
+// A block maps a run of tokens, a thread one at a time or four side by side (which for prompts mostly are one request's,
+// in one block or in two).  The offsets and lengths of their requests are brought into shared memory, those of all
+// requests where that is few, else those from the first to the last token's, which the first warps look for; every thread
+// finds the request of its tokens there.  (Between two tokens may lie more empty requests than there is room for: then the
+// offsets are searched where they are.)  Bound: latency, a chain of three to five dependent reads; for prompts writing
+// the slots.
+constexpr int kSlotRows = 1024;
+template <int PER>
 __global__ void __launch_bounds__(kThreads) k_slot_map(SlotArgs a) {
+  constexpr int kTile = PER * PER * kThreads;
   __shared__ int ends[kSlotRows + 1], length[kSlotRows];
   __shared__ int range[2];
-  const int t0 = blockIdx.x * kSlotTile, t1 = min(t0 + kSlotTile, a.T);
-  if (threadIdx.x < 64) {
-    const int which = threadIdx.x >> 5;
-    const int r = requests_before(a.off, 0, a.R, which ? t1 - 1 : t0);
-    if ((threadIdx.x & 31) == 0) range[which] = r;
+  follow();
+  const int t0 = blockIdx.x * kTile, t1 = (int)min((long long)t0 + kTile, (long long)a.T);
+  const auto find_range = [&](const int* off, int rows) {              // requests of the tile's first and last token
+    if (threadIdx.x < 64) {
+      const int which = threadIdx.x >> 5;
+      const int r = requests_before(off, 0, rows, which ? t1 - 1 : t0);
+      if ((threadIdx.x & 31) == 0) range[which] = r;
+    }
+    __syncthreads();
+  };
+  int r0 = 0, n = a.R;
+  if (a.R > kSlotRows) {
+    find_range(a.off, a.R);
+    r0 = range[0];
+    n = min(range[1], a.R - 1) - r0 + 1;                               // (off decreases against the rule: n may be anything)
   }
-  __syncthreads();
-  const int r0 = range[0], n = min(range[1], a.R - 1) - r0 + 1;        // (off decreases against the rule: n may be anything)
   const bool staged = n >= 1 && n <= kSlotRows;
   if (staged) {
-    for (int i = threadIdx.x; i <= n; i += kThreads) ends[i] = a.off[r0 + i];
-    for (int i = threadIdx.x; i < n; i += kThreads) length[i] = a.lens[r0 + i];
+#pragma unroll
+    for (int k = 0; k <= kSlotRows / kThreads; ++k)
+      if (const int i = k * kThreads + threadIdx.x; i <= n) ends[i] = a.off[r0 + i];
+#pragma unroll
+    for (int k = 0; k < kSlotRows / kThreads; ++k)
+      if (const int i = k * kThreads + threadIdx.x; i < n) length[i] = a.lens[r0 + i];
   }
   __syncthreads();
   const int* off = staged ? ends : a.off;                              // off[i + 1]: where the tokens of request i of these end
   const int* lens = staged ? length : a.lens;
   const int rows = staged ? n : a.R, first = staged ? r0 : 0;
-  const int t = t0 + 4 * threadIdx.x;
-  if (t >= t1) return;
-  int lo = 0, hi = rows;
-  while (lo < hi) {
-    const int mid = (lo + hi) >> 1;
-    if (off[mid + 1] <= t) lo = mid + 1;
-    else hi = mid;
+  int low = 0, high = rows;
+  if (PER > 1 && staged && a.R <= kSlotRows) {
+    find_range(ends, rows);
+    low = min(range[0], rows), high = max(min(range[1], rows), low);
   }
-  int v[4];
   bool bad = false;
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    v[k] = -1;
-    while (lo < rows && off[lo + 1] <= t + k) ++lo;
-    if (t + k >= t1 || lo >= rows || t + k < off[lo]) continue;
-    const long long p = (long long)lens[lo] - ((long long)off[lo + 1] - (t + k));
-    int page = -1;
-    uint32_t q = 0;
-    if (p >= 0) {
-      q = (uint32_t)p / a.block;
-      if (q < (uint32_t)a.W) page = a.table[(size_t)(first + lo) * a.W + q];
+#pragma unroll 1
+  for (int g = 0; g < PER; ++g) {
+    const int t = t0 + PER * (g * kThreads + threadIdx.x);
+    if (t >= t1) break;
+    int lo = low, hi = high;                                           // (the request of the last token is found by elimination)
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1;
+      if (off[mid + 1] <= t) lo = mid + 1;
+      else hi = mid;
     }
-    const long long at = (long long)page * a.block.d + (p - (long long)q * a.block.d);
-    if (page < 0 || at > 0x7FFFFFFFll) bad = true;
-    else v[k] = (int)at;
+    if constexpr (PER == 1) {
+      a.out[t] = slot_of(a, off, lens, first, rows, lo, t, bad);
+    } else {
+      int v[4] = {-1, -1, -1, -1};
+      bool four = false;
+      if (lo < rows && t + 4 <= t1 && off[lo] <= t && t + 3 < off[lo + 1] && a.block.d >= 4) {
+        const uint32_t left = (uint32_t)off[lo + 1] - (uint32_t)t;
+        const int n_of = lens[lo];
+        if (n_of >= 0 && (uint32_t)n_of >= left) {
+          const uint32_t p = (uint32_t)n_of - left, q = p / a.block, inside = p - q * a.block.d;
+          const bool two = inside + 3 >= a.block.d;
+          if (q + two < (uint32_t)a.W) {
+            const int* row = a.table + (size_t)(first + lo) * a.W;
+            const int page = row[q], behind = two ? row[q + 1] : page;
+            const long long at = (long long)page * a.block.d + inside, next = (long long)behind * a.block.d + inside - (two ? a.block.d : 0);
+            four = page >= 0 && behind >= 0 && at + 3 <= 0x7FFFFFFFll && next + 3 <= 0x7FFFFFFFll;
+            if (four)
+#pragma unroll
+              for (int k = 0; k < 4; ++k) v[k] = (int)(inside + k < a.block.d ? at : next) + k;
+          }
+        }
+      }
+      if (!four) {
+#pragma unroll 1
+        for (int k = 0; k < 4 && t + k < t1; ++k) {
+          while (lo < rows && off[lo + 1] <= t + k) ++lo;
+          const int x = slot_of(a, off, lens, first, rows, lo, t + k, bad);
+          if (k == 0) v[0] = x;
+          else if (k == 1) v[1] = x;
+          else if (k == 2) v[2] = x;
+          else v[3] = x;
+        }
+      }
+      if (t + 4 <= t1) *reinterpret_cast<int4*>(a.out + t) = make_int4(v[0], v[1], v[2], v[3]);
+      else for (int k = 0; t + k < t1; ++k) a.out[t + k] = v[k];
+    }
   }
   if (bad) raise_index(a.report);
-  if (t + 4 <= t1) *reinterpret_cast<int4*>(a.out + t) = make_int4(v[0], v[1], v[2], v[3]);
-  else for (int k = 0; t + k < t1; ++k) a.out[t + k] = v[k];
 }
 
+// Tokens up to which every thread takes one: a step's tokens are of a request each, so that four side by side would read
+// the table one after the other.
+constexpr int kSingleTokens = 1 << 16;
 int launch_slot_map(const ClusterLaunch& L) {
   const dev::NodeArg& table = slot(L, 0);
   SlotArgs a{report_of(L), slot_ptr<int>(L, 0), slot_ptr<int>(L, 1), slot_ptr<int>(L, 2), result_ptr<int>(L),
              table.R, table.C, (int)L.op.shape[0], divisor((uint32_t)L.op.iparam[0])};
   if (a.T == 0) return ACC_OK;
-  k_slot_map<<<(unsigned)((a.T + kSlotTile - 1) / kSlotTile), kThreads, 0, L.stream>>>(a);
-  return launched();
+  const bool single = a.T <= kSingleTokens;
+  const int tile = single ? kThreads : 16 * kThreads;
+  return launch_following(single ? k_slot_map<1> : k_slot_map<4>, dim3((unsigned)(((long long)a.T + tile - 1) / tile)), kThreads, 0, L.stream, a);
 }
 
 const Register block_table(ACC_BLOCK_TABLE, "k_block_table", no_scratch, launch_block_table);

@@ -268,6 +268,7 @@ REFUSALS = [
     (W.penalized_logits(2, 40, 3, 2, True), 6, (3, {"shape": (2, 3)}), {}, "ACC_ERR_SHAPE"),
     (W.penalized_logits(2, 40, 3, 2, True), 6, (5, {"shape": (2, 1)}), {}, "ACC_ERR_SHAPE"),
     (W.penalized_logits(2, 40, 3, 2, True), 6, (1, {"shape": (3, 3)}), {}, "ACC_ERR_SHAPE"),
+    (W.penalized_logits(2, 40, 3, 65536, True), 6, None, {}, "ACC_ERR_UNSUPPORTED"),
 ]
 
 
@@ -384,6 +385,38 @@ def test_tables_and_slots(R, Wd, block, grow):
     if grow:
         got = gpu(prog, d, into={"table": "old"})
         assert np.array_equal(got["table"], want.values[prog.id("table")])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("block", [1, 3, 4, 7, 32])
+@pytest.mark.parametrize("R", [900, 1500])
+def test_slots_of_long_prompts(R, block):
+    """So many tokens that a thread takes four side by side: of one request, of several, across blocks, the last of the batch."""
+    rng = np.random.default_rng(R + block)
+    counts = np.concatenate([rng.integers(0, 4, R - 12), rng.integers(4000, 9000, 12)])
+    rng.shuffle(counts)
+    old = rng.integers(0, 50, R)
+    lens = old + counts
+    Wd = int(-(-lens.max() // block))
+    off = np.concatenate([[0], np.cumsum(counts)])
+    d = {"lens": lens.astype(np.int32), "off": off.astype(np.int32), "table": rng.integers(0, (2 ** 31 - 1) // block - 1, (R, Wd)).astype(np.int32)}
+    T = int(off[-1]) + 6
+    assert T > 1 << 16
+    nodes = [Node("input", "i32", (R, Wd), name="table"), Node("input", "i32", (R,), name="lens"), Node("input", "i32", (R + 1,), name="off"),
+             Node("slot_map", "i32", (T,), (0, 1, 2), 3, iparam=(block,), name="slots")]
+    prog = W.Program("slots", nodes, [3])
+    row = np.repeat(np.arange(R), counts)
+    p = old[row] + np.arange(off[-1]) - off[row]
+    want = np.full(T, -1, np.int64)
+    want[:off[-1]] = d["table"][row, p // block].astype(np.int64) * block + p % block
+    assert np.array_equal(gpu(prog, d)["slots"].view(np.int32), want)
+    # the last block of one request is missing, another's number leads beyond 32 bits
+    d["table"][int(np.argmax(counts)), (lens[np.argmax(counts)] - 1) // block] = -1
+    if block > 1:
+        d["table"][row[-1], p[-1] // block] = 2 ** 31 - 1
+    slot = d["table"][row, p // block].astype(np.int64) * block + p % block
+    want[:off[-1]] = np.where((d["table"][row, p // block] < 0) | (slot >= 2 ** 31), -1, slot)
+    assert np.array_equal(gpu(prog, d, reported=True)["slots"].view(np.int32), want)
 
 
 @pytest.mark.gpu

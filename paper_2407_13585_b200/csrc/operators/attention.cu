@@ -690,30 +690,55 @@ __global__ void __launch_bounds__(kThreads, HalfShape<DP, NT, WAYS>::kResident) 
 
 // ---- fp32 --------------------------------------------------------------------------------------------------------------
 
-template <int DP>
+template <int DP, int HEADS>
 struct FloatShape {
-  static constexpr int kTokens = 8, kTile = kWarps * kTokens, kRows = 8, kWays = 1;
+  static constexpr int kTokens = 8, kTile = kWarps * kTokens, kRows = HEADS, kWays = 1;
   static constexpr int kStageBytes = 2 * kTokens * DP * 4;
-  static constexpr int kStages = DP == 64 ? 3 : 2;
-  static constexpr int kResident = DP == 256 ? 1 : DP == 128 ? 2 : 3;
-  static constexpr int kShared = kWarps * kStages * kStageBytes + kRows * DP * 4;        // (the queries behind the stages)
+  static constexpr int kStages = DP == 128 ? 2 : 3;
+  static constexpr int kResident = DP == 256 ? 1 : DP == 64 && HEADS < 8 ? 4 : 3;
+  static constexpr int kShared = kWarps * kStages * kStageBytes;
 };
 
-// The same walk with 32-bit multiplications and additions, eight heads at a time.  Scores: lane 4 t + p has every fourth
-// chunk of token t's key, each chunk used for eight heads; their sums are scattered over the four lanes, two heads to a
-// lane.  Values: a lane has four dimensions of all eight heads.
-template <int DP>
-__global__ void __launch_bounds__(kThreads) k_attention_float(AttentionArgs a) {
-  using S = FloatShape<DP>;
+// Two 32-bit numbers in one register pair, worked on by one instruction each.
+using Pair = unsigned long long;
+__device__ __forceinline__ Pair pair_of(float lo, float hi) {
+  Pair p;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(p) : "f"(lo), "f"(hi));
+  return p;
+}
+__device__ __forceinline__ float2 both_of(Pair p) {
+  float2 v;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(v.x), "=f"(v.y) : "l"(p));
+  return v;
+}
+__device__ __forceinline__ Pair fma_pair(Pair a, Pair b, Pair c) {
+  Pair d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+__device__ __forceinline__ Pair mul_pair(Pair a, Pair b) {
+  Pair d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+
+// The same walk with 32-bit multiplications and additions, two, four or eight heads at a time.  Scores: DP / 8 lanes share
+// a token, eight dimensions of all heads' queries in a lane's registers; the heads' sums are scattered over those lanes,
+// so that a lane ends up with one head's scores.  (With the queries in shared memory, read for every key, the block waits
+// for shared memory: eight heads of 128, 2 GB of keys and values 459 us.)  Values: a lane has four dimensions of all heads.
+template <int DP, int HEADS>
+__global__ void __launch_bounds__(kThreads, FloatShape<DP, HEADS>::kResident) k_attention_float(AttentionArgs a) {
+  using S = FloatShape<DP, HEADS>;
+  constexpr int LANES = DP / 8, AT_ONCE = 32 / LANES, PASSES = S::kTokens / AT_ONCE;        // lanes of a token, tokens of a pass
   constexpr int CHUNKS = DP / 4, SPLIT = CHUNKS < 32 ? 32 / CHUNKS : 1, VECS = CHUNKS / 32 > 1 ? CHUNKS / 32 : 1;
   extern __shared__ __align__(128) unsigned char shared[];
   __shared__ long long scan[kWarps];
   __shared__ Place place;
   __shared__ float ml[2 * kWarps * S::kRows];
-  __shared__ __align__(16) float weights[kWarps][8][8], falls[kWarps][8];
+  __shared__ __align__(16) float2 weights[kWarps][HEADS][8];       // each twice, for pairs of dimensions
+  __shared__ float falls[kWarps][HEADS];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   cudaTriggerProgrammaticLaunchCompletion();
-  float* query = reinterpret_cast<float*>(shared + kWarps * S::kStages * S::kStageBytes);
   Cursor<S::kTile> c = find_place<float, S::kTile>(a, &place, scan);
   int4 join = make_int4(-1, 0, 0, 0);          // (by block)
   if (c.left <= 0) {
@@ -722,10 +747,11 @@ __global__ void __launch_bounds__(kThreads) k_attention_float(AttentionArgs a) {
   }
   const unsigned char* ring = shared + warp * S::kStages * S::kStageBytes;
   const uint32_t ring_at = shared_address(ring);
-  const auto swizzle_keys = [](int row) { return (row & 1) << 2; };
   const auto plain = [](int) { return 0; };
-  const int token = lane >> 2, part = lane & 3;
-  const int head = (part & 1) * 4 + (part >> 1) * 2;         // and the one behind it: the two that this lane's sums end up with
+  const int part = lane % LANES, token = lane / LANES;        // of a pass
+  int head = 0;                                               // this lane's
+#pragma unroll
+  for (int b = 0, left = HEADS / 2; left > 0; ++b, left /= 2) head += (lane >> b & 1) * left;
   const int chunk = lane % (CHUNKS < 32 ? CHUNKS : 32), half = lane / (CHUNKS < 32 ? CHUNKS : 32);
 
   Cursor<S::kTile> next = c;
@@ -735,37 +761,41 @@ __global__ void __launch_bounds__(kThreads) k_attention_float(AttentionArgs a) {
   for (int s = 0; s < S::kStages - 1; ++s) {
     have[s] = 0;
     if (next.left > 0) {
-      have[s] = ask_for<float, DP, CHUNKS, S::kTokens>(a, next, ahead, ring_at + s * S::kStageBytes, lane, next.unit / (a.units / a.Hk), swizzle_keys, plain);
+      have[s] = ask_for<float, DP, CHUNKS, S::kTokens>(a, next, ahead, ring_at + s * S::kStageBytes, lane, next.unit / (a.units / a.Hk), plain, plain);
       next.advance(a);
       ahead = look_ahead<S::kTile, S::kTokens>(a, next, warp * S::kTokens, lane);
     }
     commit_copies();
   }
-  float o[8][VECS][4], m[2], l[2];
+  Pair o[HEADS][VECS][2];
+  Pair q[HEADS][4];
+  float m, l;
   bool fresh = true, from_start = c.tile == 0;
   int stage = 0;
   while (c.left > 0) {
     if (fresh) {
       fresh = false;
       const int per = a.units / a.Hk, head0 = c.unit % per * S::kRows, kv = c.unit / per;
-      for (int i = threadIdx.x; i < 8 * DP; i += kThreads) {
-        const int h = i / DP, d = i % DP;
-        query[i] = head0 + h < a.group && d < a.D ? static_cast<const float*>(a.q)[((size_t)c.b * a.Hq + (size_t)kv * a.group + head0 + h) * a.D + d] : 0.0f;
+#pragma unroll
+      for (int h = 0; h < HEADS; ++h) {
+        const float4* from = reinterpret_cast<const float4*>(static_cast<const float*>(a.q) + ((size_t)c.b * a.Hq + (size_t)kv * a.group + head0 + h) * a.D);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int at = part + i * LANES;
+          const float4 x = head0 + h < a.group && at * 4 < a.D ? from[at] : make_float4(0, 0, 0, 0);
+          q[h][2 * i] = pair_of(x.x, x.y), q[h][2 * i + 1] = pair_of(x.z, x.w);
+        }
+#pragma unroll
+        for (int v = 0; v < VECS; ++v) o[h][v][0] = o[h][v][1] = 0;
       }
-#pragma unroll
-      for (int h = 0; h < 8; ++h)
-#pragma unroll
-        for (int v = 0; v < VECS; ++v) o[h][v][0] = o[h][v][1] = o[h][v][2] = o[h][v][3] = 0;
-      m[0] = m[1] = -INFINITY;
-      l[0] = l[1] = 0;
-      __syncthreads();
+      m = -INFINITY, l = 0;
     }
     uint32_t got = 0;
     {
       int to = stage + S::kStages - 1;
       if (to >= S::kStages) to -= S::kStages;
       if (next.left > 0) {
-        got = ask_for<float, DP, CHUNKS, S::kTokens>(a, next, ahead, ring_at + to * S::kStageBytes, lane, next.unit / (a.units / a.Hk), swizzle_keys, plain);
+        got = ask_for<float, DP, CHUNKS, S::kTokens>(a, next, ahead, ring_at + to * S::kStageBytes, lane, next.unit / (a.units / a.Hk), plain, plain);
         next.advance(a);
         ahead = look_ahead<S::kTile, S::kTokens>(a, next, warp * S::kTokens, lane);
       }
@@ -778,80 +808,72 @@ __global__ void __launch_bounds__(kThreads) k_attention_float(AttentionArgs a) {
     for (int s = 0; s + 1 < S::kStages - 1; ++s) have[s] = have[s + 1];
     have[S::kStages - 2] = got;
     if (valid) {
-      const float4* keys = reinterpret_cast<const float4*>(ring + stage * S::kStageBytes) + token * CHUNKS;
-      const float4* values = reinterpret_cast<const float4*>(ring + stage * S::kStageBytes) + S::kTokens * CHUNKS;
-      float s[8];
+      const ulonglong2* keys = reinterpret_cast<const ulonglong2*>(ring + stage * S::kStageBytes);
+      const ulonglong2* values = keys + S::kTokens * CHUNKS;
+      float s[PASSES], top = -INFINITY;
 #pragma unroll
-      for (int h = 0; h < 8; ++h) s[h] = 0;
-#pragma unroll 4
-      for (int i = 0; i < CHUNKS / 4; ++i) {
-        const float4 k = keys[(i * 4 + part) ^ ((token & 1) << 2)];
+      for (int j = 0; j < PASSES; ++j) {
+        const int t = j * AT_ONCE + token;
+        const ulonglong2 k0 = keys[t * CHUNKS + part], k1 = keys[t * CHUNKS + part + LANES];
+        float x[HEADS];
 #pragma unroll
-        for (int h = 0; h < 8; ++h) {
-          const float4 x = reinterpret_cast<const float4*>(query)[h * CHUNKS + i * 4 + part];
-          s[h] = fmaf(k.x, x.x, fmaf(k.y, x.y, fmaf(k.z, x.z, fmaf(k.w, x.w, s[h]))));
+        for (int h = 0; h < HEADS; ++h) {
+          const float2 y = both_of(fma_pair(k1.y, q[h][3], fma_pair(k1.x, q[h][2], fma_pair(k0.y, q[h][1], mul_pair(k0.x, q[h][0])))));
+          x[h] = y.x + y.y;
         }
-      }
-      float t4[4], t2[2];
+        int left = HEADS;                      // heads halved between the lanes of pairs, then sums alone
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float other = __shfl_xor_sync(~0u, part & 1 ? s[i] : s[i + 4], 1);
-        t4[i] = (part & 1 ? s[i + 4] : s[i]) + other;
+        for (int b = 1; b < LANES; b <<= 1) {
+          if (left > 1) {
+            left /= 2;
+#pragma unroll
+            for (int i = 0; i < left; ++i) {
+              const float other = __shfl_xor_sync(~0u, lane & b ? x[i] : x[i + left], b);
+              x[i] = (lane & b ? x[i + left] : x[i]) + other;
+            }
+          } else x[0] += __shfl_xor_sync(~0u, x[0], b);
+        }
+        const bool is = valid >> t & 1;
+        s[j] = is ? x[0] * a.scale_log2 : -INFINITY;
+        top = fmaxf(top, is ? fmaxf(s[j], -FLT_MAX) : -INFINITY);
       }
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const float other = __shfl_xor_sync(~0u, part & 2 ? t4[i] : t4[i + 2], 2);
-        t2[i] = (part & 2 ? t4[i + 2] : t4[i]) + other;
-      }
-      const bool is = valid >> token & 1;
-      float top[2];
-      bool rises = false;
+      for (int d = LANES; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
+      top = fmaxf(top, m);
+      const bool rises = __any_sync(~0u, top > m);
+      const float fall = power2(m - top);
+      m = top;
+      l *= fall;
+      const bool writes = part < HEADS;                       // (further lanes of a token hold the same again)
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        t2[i] = is ? t2[i] * a.scale_log2 : -INFINITY;
-        top[i] = is ? fmaxf(t2[i], -FLT_MAX) : -INFINITY;
-#pragma unroll
-        for (int d = 4; d < 32; d <<= 1) top[i] = fmaxf(top[i], __shfl_xor_sync(~0u, top[i], d));
-        top[i] = fmaxf(top[i], m[i]);
-        rises = rises || top[i] > m[i];
+      for (int j = 0; j < PASSES; ++j) {
+        const float w = power2(s[j] - top);
+        l += w;
+        if (writes) weights[warp][head][j * AT_ONCE + token] = make_float2(w, w);
       }
-      rises = __any_sync(~0u, rises);
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const float fall = power2(m[i] - top[i]);
-        const float w = power2(t2[i] - top[i]);
-        l[i] = fmaf(l[i], fall, w);
-        m[i] = top[i];
-        weights[warp][head + i][token] = w;
-        if (token == 0) falls[warp][head + i] = fall;
-      }
+      if (lane < HEADS) falls[warp][head] = fall;
       __syncwarp();
 #pragma unroll
-      for (int h = 0; h < 8; ++h) {
+      for (int h = 0; h < HEADS; ++h) {
         if (rises) {
-          const float fall = falls[warp][h];
+          const Pair fall = pair_of(falls[warp][h], falls[warp][h]);
 #pragma unroll
-          for (int v = 0; v < VECS; ++v) o[h][v][0] *= fall, o[h][v][1] *= fall, o[h][v][2] *= fall, o[h][v][3] *= fall;
+          for (int v = 0; v < VECS; ++v) o[h][v][0] = mul_pair(o[h][v][0], fall), o[h][v][1] = mul_pair(o[h][v][1], fall);
         }
       }
-      constexpr int QUADS = 2 / SPLIT;                       // fours of tokens that a lane goes through
 #pragma unroll
-      for (int f = 0; f < QUADS; ++f) {
-        const int t0 = (SPLIT == 2 ? half : f) * 4;
-        float4 w[8];
+      for (int f = 0; f < 4 / SPLIT; ++f) {                  // tokens two by two
+        const int t0 = ((SPLIT == 2 ? half * 2 : 0) + f) * 2;
+        ulonglong2 w[HEADS];
 #pragma unroll
-        for (int h = 0; h < 8; ++h) w[h] = *reinterpret_cast<const float4*>(&weights[warp][h][t0]);
+        for (int h = 0; h < HEADS; ++h) w[h] = *reinterpret_cast<const ulonglong2*>(&weights[warp][h][t0]);
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
+        for (int v = 0; v < VECS; ++v) {
+          const ulonglong2 x = values[t0 * CHUNKS + chunk + v * 32], y = values[(t0 + 1) * CHUNKS + chunk + v * 32];
 #pragma unroll
-          for (int v = 0; v < VECS; ++v) {
-            const float4 x = values[(t0 + t) * CHUNKS + chunk + v * 32];
-#pragma unroll
-            for (int h = 0; h < 8; ++h) {
-              const float y = t == 0 ? w[h].x : t == 1 ? w[h].y : t == 2 ? w[h].z : w[h].w;
-              o[h][v][0] = fmaf(y, x.x, o[h][v][0]), o[h][v][1] = fmaf(y, x.y, o[h][v][1]);
-              o[h][v][2] = fmaf(y, x.z, o[h][v][2]), o[h][v][3] = fmaf(y, x.w, o[h][v][3]);
-            }
+          for (int h = 0; h < HEADS; ++h) {
+            o[h][v][0] = fma_pair(w[h].y, y.x, fma_pair(w[h].x, x.x, o[h][v][0]));
+            o[h][v][1] = fma_pair(w[h].y, y.y, fma_pair(w[h].x, x.y, o[h][v][1]));
           }
         }
       }
@@ -864,23 +886,21 @@ __global__ void __launch_bounds__(kThreads) k_attention_float(AttentionArgs a) {
       float* sums = reinterpret_cast<float*>(shared + used * S::kStageBytes);      // through the stage just read
       constexpr int kStride = S::kStages * S::kStageBytes / 4;
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-#pragma unroll
-        for (int d = 4; d < 32; d <<= 1) l[i] += __shfl_xor_sync(~0u, l[i], d);
-        if (token == 0) {
-          ml[warp * S::kRows + head + i] = m[i];
-          ml[(kWarps + warp) * S::kRows + head + i] = l[i];
-        }
+      for (int d = LANES; d < 32; d <<= 1) l += __shfl_xor_sync(~0u, l, d);
+      if (lane < HEADS) {
+        ml[warp * S::kRows + head] = m;
+        ml[(kWarps + warp) * S::kRows + head] = l;
       }
 #pragma unroll
-      for (int h = 0; h < 8; ++h)
+      for (int h = 0; h < HEADS; ++h)
 #pragma unroll
         for (int v = 0; v < VECS; ++v) {
+          const float2 lo = both_of(o[h][v][0]), hi = both_of(o[h][v][1]);
+          float x[4] = {lo.x, lo.y, hi.x, hi.y};
           if constexpr (SPLIT == 2)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) o[h][v][i] += __shfl_xor_sync(~0u, o[h][v][i], 16);
-          if (half == 0)
-            *reinterpret_cast<float4*>(sums + warp * kStride + h * DP + (chunk + v * 32) * 4) = make_float4(o[h][v][0], o[h][v][1], o[h][v][2], o[h][v][3]);
+            for (int i = 0; i < 4; ++i) x[i] += __shfl_xor_sync(~0u, x[i], 16);
+          if (half == 0) *reinterpret_cast<float4*>(sums + warp * kStride + h * DP + (chunk + v * 32) * 4) = make_float4(x[0], x[1], x[2], x[3]);
         }
       __syncthreads();
       finish_unit<float, DP, S::kRows, false>(a, c.b, c.unit / per, c.unit % per * S::kRows, from_start, to_end, sums, kStride, ml);
@@ -941,7 +961,7 @@ int run(const ClusterLaunch& L, K kernel, std::atomic<uint64_t>& allowed) {
   }
   const int rc = allow_shared(kernel, S::kShared, allowed);
   if (rc != ACC_OK) return rc;
-  a.join_rows = (long long)a.B * a.units * kManyRecords < grid ? 1 : 8;
+  a.join_rows = (long long)a.B * a.units * kManyRecords < grid ? 1 : std::min(8, S::kRows * S::kWays);
   // (not launched early: beside the kernel before it an SM is divided for less shared memory, and keeps to that while the
   // blocks that did fit run; 31 windows of 4096 tokens, back to back: 101 us, launched early 154)
   kernel<<<grid, kThreads, S::kShared, L.stream>>>(a);
@@ -977,9 +997,16 @@ template <class F>
 auto choose(const ClusterLaunch& L, F f) {
   const int D = (int)L.op.iparam[1];
   if (L.op.dtype == ACC_F32) {
-    if (D <= 64) return f(float{}, std::integral_constant<int, 64>{}, FloatShape<64>{}, k_attention_float<64>);
-    if (D <= 128) return f(float{}, std::integral_constant<int, 128>{}, FloatShape<128>{}, k_attention_float<128>);
-    return f(float{}, std::integral_constant<int, 256>{}, FloatShape<256>{}, k_attention_float<256>);
+    const auto heads = [&](auto dp) {
+      constexpr int DP = decltype(dp)::value;
+      const int group = (int)(L.op.shape[1] / std::max(slot(L, 1).C, 1));
+      if (group <= 2) return f(float{}, dp, FloatShape<DP, 2>{}, k_attention_float<DP, 2>);
+      if (group <= 4) return f(float{}, dp, FloatShape<DP, 4>{}, k_attention_float<DP, 4>);
+      return f(float{}, dp, FloatShape<DP, 8>{}, k_attention_float<DP, 8>);
+    };
+    if (D <= 64) return heads(std::integral_constant<int, 64>{});
+    if (D <= 128) return heads(std::integral_constant<int, 128>{});
+    return heads(std::integral_constant<int, 256>{});
   }
   return L.op.dtype == ACC_F16 ? choose_half<__half>(L, f) : choose_half<__nv_bfloat16>(L, f);
 }

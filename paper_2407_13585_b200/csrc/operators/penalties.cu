@@ -61,6 +61,9 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_penalize(PenaltyArg
   }
 #pragma unroll
   for (int k = 0; k < kHeld; ++k) held[k] = k * THREADS + (int)threadIdx.x < a.L ? tokens[k * THREADS + threadIdx.x] : -1;
+  // the warp that goes through the biases has the last of them at hand
+  const int bias_lane = (int)threadIdx.x - (THREADS - 32), last_bias = (a.K - 1) / 32 * 32 + bias_lane;
+  const int last_id = a.K > 0 && bias_lane >= 0 && last_bias < a.K ? ids[last_bias] : -1;
   const uint32_t width = v1 - v0;
   if (marks) {
     for (int i = threadIdx.x; i < kCols / 32; i += THREADS) touched[i] = 0;
@@ -120,11 +123,10 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_penalize(PenaltyArg
   for (int k = 0; k < kHeld; ++k) note(held[k], k * THREADS + threadIdx.x);
 #pragma unroll 4
   for (int i = kHeld * THREADS + threadIdx.x; i < a.L; i += THREADS) note(tokens[i], i);
-  if (threadIdx.x < 32 && a.K > 0) {                           // from the last bias to the first, 32 at a time
-    const int lane = threadIdx.x;
-    int k = (a.K - 1) / 32 * 32 + lane;
-    int v = k < a.K ? ids[k] : -1;
-    for (; k >= lane; k -= 32) {
+  if (bias_lane >= 0 && a.K > 0) {                             // from the last bias to the first, 32 at a time
+    const int lane = bias_lane;
+    int v = last_id;
+    for (int k = last_bias; k >= lane; k -= 32) {
       const int before = k >= 32 + lane ? ids[k - 32] : -1;
       const bool mine = (uint32_t)(v - v0) < width;
       const uint32_t same = __match_any_sync(~0u, mine ? v : -1 - lane);

@@ -31,8 +31,8 @@ constexpr int kUnitsPerLane = 4;
 template <int BYTES>
 __global__ void __launch_bounds__(128) k_put_rows(RowArgs a) {
   using U = typename Unit<BYTES>::type;
-  // behind the kernels that settle owners only they are waited for, and only once the row is on its way: they were not
-  // launched before what the slots and rows come from had finished
+  // behind the kernel that settles owners it is waited for only once the row is on its way: that kernel did not begin
+  // before all that slots and rows come from had finished
   if (a.owner) cudaTriggerProgrammaticLaunchCompletion();
   else follow();
   const int lane = threadIdx.x & 31;
@@ -66,15 +66,19 @@ __global__ void __launch_bounds__(128) k_put_rows(RowArgs a) {
     if (first + 32 * k < a.units) to[first + 32 * k] = v[k];
 }
 
-__global__ void __launch_bounds__(256) k_clear_owners(const int* slots, int* owner, int T, int S) {
+// owner[s] = the last row for slot s, without clearing the array first: a number that is no row for this slot is nobody's,
+// and one that is a row for it is an owner like any other, wherever it comes from.
+__global__ void __launch_bounds__(256) k_settle_owners(const int* slots, int* owner, int T, int S) {
   cudaTriggerProgrammaticLaunchCompletion();
   const int t = blockIdx.x * 256 + threadIdx.x;
-  if (t < T && slots[t] >= 0 && slots[t] < S) owner[slots[t]] = -1;
-}
-__global__ void __launch_bounds__(256) k_last_owner(const int* slots, int* owner, int T, int S) {
-  follow();
-  const int t = blockIdx.x * 256 + threadIdx.x;
-  if (t < T && slots[t] >= 0 && slots[t] < S) atomicMax(owner + slots[t], t);
+  const int slot = t < T ? slots[t] : -1;
+  if (slot < 0 || slot >= S) return;
+  int old = *reinterpret_cast<volatile int*>(owner + slot);
+  while (!((uint32_t)old < (uint32_t)T && old >= t && slots[old] == slot)) {
+    const int seen = atomicCAS(owner + slot, old, t);
+    if (seen == old) break;
+    old = seen;
+  }
 }
 
 __global__ void __launch_bounds__(256) k_copy_array(const uint4* from, uint4* to, size_t vectors, size_t bytes) {
@@ -88,8 +92,9 @@ __global__ void __launch_bounds__(256) k_copy_array(const uint4* from, uint4* to
 }
 
 // Up to this many rows every row looks at the slots behind it (4 T^2 / 2 bytes, from L1 and L2), one launch; beyond, the
-// slots' owners are settled first, three launches.
-constexpr int kRowsThatLook = 4096;
+// slots' owners are settled first, two launches (rows of 2 KB, twice: 200 10.2 us looked, 12.3 settled; 500 14.3 and 12.3;
+// 8000 47 and 19).
+constexpr int kRowsThatLook = 256;
 
 int64_t put_rows_scratch(const ClusterLaunch& L) { return slot(L, 1).C > kRowsThatLook ? 4 * L.op.shape[0] : 0; }
 
@@ -111,9 +116,9 @@ int launch_put_rows(const ClusterLaunch& L) {
     if (a.T > kRowsThatLook) {
       a.owner = reinterpret_cast<int*>(L.scratch);
       // (launched like any other kernel: it begins when everything before it has finished)
-      k_clear_owners<<<(a.T + 255) / 256, 256, 0, L.stream>>>(a.slots, a.owner, a.T, a.S);
-      if ((rc = launched()) == ACC_OK) rc = launch_following(k_last_owner, dim3((a.T + 255) / 256), 256, 0, L.stream, a.slots, a.owner, a.T, a.S);
-      launches += 2;
+      k_settle_owners<<<(a.T + 255) / 256, 256, 0, L.stream>>>(a.slots, a.owner, a.T, a.S);
+      rc = launched();
+      ++launches;
     }
     const int unit = row_bytes % 16 == 0 ? 16 : row_bytes % 4 == 0 ? 4 : 2;
     a.units = (int)(row_bytes / unit);

@@ -15,37 +15,42 @@ struct TableArgs {
   Divisor block, width;
 };
 
+// Sums that stay at 2^31 - 1 once they get there: more than any list is long.
+__device__ __forceinline__ uint32_t add_up_to(uint32_t a, uint32_t b) { return min(a + b, 0x7FFFFFFFu); }
+
 // Of v: the sum over the threads before this one, and over all; of w the sum over all.  (kThreads threads.)
 struct Scan {
-  long long before, all, all_w;
+  uint32_t before, all, all_w;
 };
-__device__ __forceinline__ Scan block_scan(long long v, long long w, long long (*warp_sums)[2]) {
+__device__ __forceinline__ Scan block_scan(uint32_t v, uint32_t w, uint32_t (*warp_sums)[2]) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  long long incl = v;
+  uint32_t incl = v;
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
-    const long long below = __shfl_up_sync(~0u, incl, d);
-    w += __shfl_xor_sync(~0u, w, d);
-    if (lane >= d) incl += below;
+    const uint32_t below = __shfl_up_sync(~0u, incl, d);
+    w = add_up_to(w, __shfl_xor_sync(~0u, w, d));
+    if (lane >= d) incl = add_up_to(incl, below);
   }
+  const uint32_t above = __shfl_up_sync(~0u, incl, 1);
   if (lane == 31) warp_sums[warp][0] = incl, warp_sums[warp][1] = w;
   __syncthreads();
-  Scan r{incl - v, 0, 0};
+  Scan r{lane == 0 ? 0 : above, 0, 0};
+  uint32_t ahead = 0;
 #pragma unroll
   for (int k = 0; k < kThreads / 32; ++k) {
-    if (k < warp) r.before += warp_sums[k][0];
-    r.all += warp_sums[k][0];
-    r.all_w += warp_sums[k][1];
+    if (k == warp) ahead = r.all;
+    r.all = add_up_to(r.all, warp_sums[k][0]);
+    r.all_w = add_up_to(r.all_w, warp_sums[k][1]);
   }
+  r.before = add_up_to(r.before, ahead);
   __syncthreads();
   return r;
 }
 
-__device__ __noinline__ int table_entry(const TableArgs& a, int f, int j, int first, int kept, int need) {
-  if (j >= need) return -1;
-  if (j < kept) return a.old ? a.old[f] : -1;
-  const long long at = (long long)first + j - kept;
-  return at < a.N ? a.free[at] : -1;
+// An entry of a row {kept, end, from}: its first `kept` entries are the old row's, entry j in kept <= j < end is
+// free[from + j], the others are -1.
+__device__ __noinline__ int table_entry(const TableArgs& a, int f, int j, int4 row) {
+  return j < row.x ? (a.old ? a.old[f] : -1) : j < row.y ? a.free[row.z + j] : -1;
 }
 
 // table[r, j] = old[r, j] | free[base_r + j - had_r] | -1 with base_r the blocks that earlier requests took.  A block
@@ -55,56 +60,57 @@ __device__ __noinline__ int table_entry(const TableArgs& a, int f, int j, int fi
 // R < a.tile.  kTableRows rows at most: where they are shorter than eight elements a block takes fewer elements.
 constexpr int kTableTile = 8192, kTableRows = 1024;
 __global__ void __launch_bounds__(kThreads) k_block_table(TableArgs a) {
-  __shared__ long long warp_sums[kThreads / 32][2];
-  __shared__ int first_free[kTableRows + 2], had[kTableRows + 2], has[kTableRows + 2];
+  __shared__ uint32_t warp_sums[kThreads / 32][2];
+  __shared__ int4 rows[kTableRows + 2];                       // kept, end, from (see table_entry)
   follow();
   const int f0 = blockIdx.x * a.tile, f1 = (int)min((long long)f0 + a.tile, (long long)a.R * a.W);
   const int r0 = (uint32_t)f0 / a.width, r1 = (uint32_t)(f1 - 1) / a.width + 1;
   const auto length = [&](int row) { return row < r1 ? a.lens[row] : 0; };
   const auto old_length = [&](int row) { return row < r1 && a.old_lens ? a.old_lens[row] : 0; };
   int len = length(r0 + threadIdx.x), old_len = old_length(r0 + threadIdx.x);
-  long long earlier = 0;
+  uint32_t earlier = 0;
 #pragma unroll 4
-  for (int r = threadIdx.x; r < r0; r += kThreads) earlier += max(blocks_of(a.lens[r], a.block) - (a.old_lens ? blocks_of(a.old_lens[r], a.block) : 0), 0);
-  long long base = 0;
+  for (int r = threadIdx.x; r < r0; r += kThreads)
+    earlier = add_up_to(earlier, max(blocks_of(a.lens[r], a.block) - (a.old_lens ? blocks_of(a.old_lens[r], a.block) : 0), 0));
+  uint32_t base = 0;
   for (int r = r0; r < r1; r += kThreads) {
     const int row = r + threadIdx.x;
     if (r > r0) len = length(row), old_len = old_length(row);
-    const int need = blocks_of(len, a.block), kept = blocks_of(old_len, a.block), taken = max(need - kept, 0);
+    const int need = blocks_of(len, a.block), had = blocks_of(old_len, a.block), taken = max(need - had, 0);
     const Scan s = block_scan(taken, r == r0 ? earlier : 0, warp_sums);
-    base += s.all_w;
+    base = add_up_to(base, s.all_w);
     if (row < r1) {
-      const long long start = base + s.before;
-      first_free[row - r0] = (int)min(start, (long long)a.N);
-      had[row - r0] = kept;
-      has[row - r0] = need;
-      if (len < 0 || old_len < 0 || need > a.W || start + taken > a.N) raise_index(a.report);
+      const uint32_t start = add_up_to(base, s.before);
+      // the list may end inside the row, or before it; from + j < N for all j < end
+      const int from = (int)min(start, (uint32_t)a.N) - had;
+      rows[row - r0] = make_int4(min(had, need), (int)min((long long)need, (long long)a.N - from), from, 0);
+      if (len < 0 || old_len < 0 || need > a.W || add_up_to(start, taken) > (uint32_t)a.N) raise_index(a.report);
     }
-    base += s.all;
+    base = add_up_to(base, s.all);
   }
   __syncthreads();
+  int f = f0 + 4 * threadIdx.x, r = (uint32_t)f / a.width, j = f - r * a.W;
 #pragma unroll 4
-  for (int f = f0 + 4 * threadIdx.x; f < f1; f += 4 * kThreads) {
-    const int r = (uint32_t)f / a.width, j = f - r * a.W;
-    if (f + 4 > f1 || j + 4 > a.W) {
-      for (int k = 0, row = r - r0, at = j; k < 4 && f + k < f1; ++k) {
-        a.out[f + k] = table_entry(a, f + k, at, first_free[row], had[row], has[row]);
-        if (++at == a.W) { at = 0; ++row; }
+  for (; f < f1; f += 4 * kThreads) {
+    const int4 row = rows[min(r - r0, kTableRows + 1)];
+    if (f + 4 <= f1 && j + 4 <= a.W) {                         // four of one row
+      int4 v = make_int4(-1, -1, -1, -1);
+      if (j < row.x && a.old) v = *reinterpret_cast<const int4*>(a.old + f);
+      if (j + 4 > row.x) {
+        if (j >= row.x) v.x = j < row.y ? a.free[row.z + j] : -1;
+        if (j + 1 >= row.x) v.y = j + 1 < row.y ? a.free[row.z + j + 1] : -1;
+        if (j + 2 >= row.x) v.z = j + 2 < row.y ? a.free[row.z + j + 2] : -1;
+        v.w = j + 3 < row.y ? a.free[row.z + j + 3] : -1;
       }
-      continue;
+      *reinterpret_cast<int4*>(a.out + f) = v;
+    } else {
+      for (int k = 0, at = j, of = r - r0; k < 4 && f + k < f1; ++k) {
+        a.out[f + k] = table_entry(a, f + k, at, rows[of]);
+        if (++at == a.W) { at = 0; ++of; }
+      }
     }
-    // four of one row: what is kept comes in one piece
-    const int need = has[r - r0], kept = min(had[r - r0], need), from = first_free[r - r0] - had[r - r0];
-    int4 x = make_int4(-1, -1, -1, -1);
-    if (a.old && j < kept) x = *reinterpret_cast<const int4*>(a.old + f);
-    int v[4] = {x.x, x.y, x.z, x.w};
-    if (j + 4 > kept) {
-      const int end = (int)min((long long)need, (long long)a.N - from);        // where the list ends
-#pragma unroll
-      for (int k = 0; k < 4; ++k)
-        if (j + k >= kept) v[k] = j + k < end ? a.free[from + j + k] : -1;
-    }
-    *reinterpret_cast<int4*>(a.out + f) = make_int4(v[0], v[1], v[2], v[3]);
+    j += 4 * kThreads;
+    if (j >= a.W) r = (uint32_t)(f + 4 * kThreads) / a.width, j = f + 4 * kThreads - r * a.W;
   }
 }
 
@@ -163,8 +169,8 @@ __device__ __forceinline__ int slot_of(const SlotArgs& a, const int* off, const 
   return (int)at;
 }
 
-// A block maps a run of tokens, a thread one at a time or four side by side (which for prompts mostly are one request's,
-// in one block or in two).  The offsets and lengths of their requests are brought into shared memory, those of all
+// A block maps a run of tokens, a thread one, four or sixteen side by side (which for prompts mostly are one request's, in
+// one block or two where blocks are no shorter).  The offsets and lengths of their requests are brought into shared memory, those of all
 // requests where that is few, else those from the first to the last token's, which the first warps look for; every thread
 // finds the request of its tokens there.  (Between two tokens may lie more empty requests than there is room for: then the
 // offsets are searched where they are.)  Bound: latency, a chain of three to five dependent reads; for prompts writing
@@ -172,7 +178,7 @@ __device__ __forceinline__ int slot_of(const SlotArgs& a, const int* off, const 
 constexpr int kSlotRows = 1024;
 template <int PER>
 __global__ void __launch_bounds__(kThreads) k_slot_map(SlotArgs a) {
-  constexpr int kTile = PER * PER * kThreads;
+  constexpr int kTile = PER * kThreads;
   __shared__ int ends[kSlotRows + 1], length[kSlotRows];
   __shared__ int range[2];
   follow();
@@ -210,67 +216,58 @@ __global__ void __launch_bounds__(kThreads) k_slot_map(SlotArgs a) {
     low = min(range[0], rows), high = max(min(range[1], rows), low);
   }
   bool bad = false;
-#pragma unroll 1
-  for (int g = 0; g < PER; ++g) {
-    const int t = t0 + PER * (g * kThreads + threadIdx.x);
-    if (t >= t1) break;
-    int lo = low, hi = high;                                           // (the request of the last token is found by elimination)
-    while (lo < hi) {
-      const int mid = (lo + hi) >> 1;
-      if (off[mid + 1] <= t) lo = mid + 1;
-      else hi = mid;
-    }
-    if constexpr (PER == 1) {
-      a.out[t] = slot_of(a, off, lens, first, rows, lo, t, bad);
-    } else {
-      int v[4] = {-1, -1, -1, -1};
-      bool four = false;
-      if (lo < rows && t + 4 <= t1 && off[lo] <= t && t + 3 < off[lo + 1] && a.block.d >= 4) {
-        const uint32_t left = (uint32_t)off[lo + 1] - (uint32_t)t;
-        const int n_of = lens[lo];
-        if (n_of >= 0 && (uint32_t)n_of >= left) {
-          const uint32_t p = (uint32_t)n_of - left, q = p / a.block, inside = p - q * a.block.d;
-          const bool two = inside + 3 >= a.block.d;
-          if (q + two < (uint32_t)a.W) {
-            const int* row = a.table + (size_t)(first + lo) * a.W;
-            const int page = row[q], behind = two ? row[q + 1] : page;
-            const long long at = (long long)page * a.block.d + inside, next = (long long)behind * a.block.d + inside - (two ? a.block.d : 0);
-            four = page >= 0 && behind >= 0 && at + 3 <= 0x7FFFFFFFll && next + 3 <= 0x7FFFFFFFll;
-            if (four)
+  const int t = t0 + PER * threadIdx.x;
+  if (t >= t1) return;
+  int lo = low, hi = high;                                             // (the request of the last token is found by elimination)
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (off[mid + 1] <= t) lo = mid + 1;
+    else hi = mid;
+  }
+  if constexpr (PER == 1) {
+    a.out[t] = slot_of(a, off, lens, first, rows, lo, t, bad);
+  } else {
+    // all of one request, in one block or in two
+    bool one = lo < rows && t + PER <= t1 && off[lo] <= t && t + PER <= off[lo + 1] && a.block.d >= PER && lens[lo] >= 0;
+    if (one) {
+      const uint32_t left = (uint32_t)off[lo + 1] - (uint32_t)t, p = (uint32_t)lens[lo] - left;
+      const uint32_t q = p / a.block, inside = p - q * a.block.d, here = a.block.d - inside;       // tokens of the first block
+      const bool two = here < PER;
+      one = (uint32_t)lens[lo] >= left && q + two < (uint32_t)a.W;
+      const int* row = a.table + (size_t)(first + lo) * a.W + q;
+      const int page = one ? row[0] : -1, behind = one && two ? row[1] : page;
+      const long long at = (long long)page * a.block.d + inside, next = two ? (long long)behind * a.block.d - here : at;
+      one = one && page >= 0 && behind >= 0 && at + PER <= 0x7FFFFFFFll && next + PER <= 0x7FFFFFFFll;
+      if (one) {
+        const int v0 = (int)at, v1 = (int)next;
+        int4* to = reinterpret_cast<int4*>(a.out + t);
 #pragma unroll
-              for (int k = 0; k < 4; ++k) v[k] = (int)(inside + k < a.block.d ? at : next) + k;
-          }
-        }
+        for (int k = 0; k < PER; k += 4)
+          to[k / 4] = make_int4((k < here ? v0 : v1) + k, (k + 1 < here ? v0 : v1) + k + 1, (k + 2 < here ? v0 : v1) + k + 2, (k + 3 < here ? v0 : v1) + k + 3);
       }
-      if (!four) {
+    }
+    if (!one) {
 #pragma unroll 1
-        for (int k = 0; k < 4 && t + k < t1; ++k) {
-          while (lo < rows && off[lo + 1] <= t + k) ++lo;
-          const int x = slot_of(a, off, lens, first, rows, lo, t + k, bad);
-          if (k == 0) v[0] = x;
-          else if (k == 1) v[1] = x;
-          else if (k == 2) v[2] = x;
-          else v[3] = x;
-        }
+      for (int k = 0; k < PER && t + k < t1; ++k) {
+        while (lo < rows && off[lo + 1] <= t + k) ++lo;
+        a.out[t + k] = slot_of(a, off, lens, first, rows, lo, t + k, bad);
       }
-      if (t + 4 <= t1) *reinterpret_cast<int4*>(a.out + t) = make_int4(v[0], v[1], v[2], v[3]);
-      else for (int k = 0; t + k < t1; ++k) a.out[t + k] = v[k];
     }
   }
   if (bad) raise_index(a.report);
 }
 
-// Tokens up to which every thread takes one: a step's tokens are of a request each, so that four side by side would read
-// the table one after the other.
+// Tokens up to which every thread takes one: a step's tokens are of a request each, so that sixteen side by side would
+// read the table one after the other.
 constexpr int kSingleTokens = 1 << 16;
 int launch_slot_map(const ClusterLaunch& L) {
   const dev::NodeArg& table = slot(L, 0);
   SlotArgs a{report_of(L), slot_ptr<int>(L, 0), slot_ptr<int>(L, 1), slot_ptr<int>(L, 2), result_ptr<int>(L),
              table.R, table.C, (int)L.op.shape[0], divisor((uint32_t)L.op.iparam[0])};
   if (a.T == 0) return ACC_OK;
-  const bool single = a.T <= kSingleTokens;
-  const int tile = single ? kThreads : 16 * kThreads;
-  return launch_following(single ? k_slot_map<1> : k_slot_map<4>, dim3((unsigned)(((long long)a.T + tile - 1) / tile)), kThreads, 0, L.stream, a);
+  const int per = a.T <= kSingleTokens ? 1 : a.block.d >= 16 ? 16 : 4;
+  const int tile = per * kThreads;
+  return launch_following(per == 1 ? k_slot_map<1> : per == 4 ? k_slot_map<4> : k_slot_map<16>, dim3((unsigned)(((long long)a.T + tile - 1) / tile)), kThreads, 0, L.stream, a);
 }
 
 const Register block_table(ACC_BLOCK_TABLE, "k_block_table", no_scratch, launch_block_table);

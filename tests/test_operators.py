@@ -457,7 +457,7 @@ def _put_program(S, C, T, dtype):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["f32", "i32", "u32", "f16", "bf16"])
-@pytest.mark.parametrize("S,C,T", [(1, 1, 1), (5, 3, 0), (40, 8, 33), (300, 1, 200), (64, 1000, 65), (50, 1027, 40), (3000, 24, 4096), (3000, 24, 4097),
+@pytest.mark.parametrize("S,C,T", [(1, 1, 1), (5, 3, 0), (40, 8, 33), (300, 1, 200), (64, 1000, 65), (50, 1027, 40), (3000, 24, 256), (3000, 24, 257), (3000, 24, 4097),
                                    (700, 5, 9001), (0, 4, 3)])
 def test_put_rows(S, C, T, dtype):
     rng = np.random.default_rng(S + C + T)

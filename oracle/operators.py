@@ -167,9 +167,8 @@ def penalize(nd, xs):
                     x[b, t] += add
                     mag[b, t] += abs(add)
         if mask.shape[1]:
-            for v in range(V):
-                if not (int(mask[b, v // 32]) >> (v % 32)) & 1:
-                    x[b, v] = -np.inf
+            v = np.arange(V)
+            x[b, (mask[b, v // 32] >> (v % 32).astype(np.uint32)) & 1 == 0] = -np.inf
     return x, mag, bad
 
 

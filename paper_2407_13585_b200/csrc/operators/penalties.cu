@@ -19,7 +19,28 @@ struct PenaltyArgs {
   void* out;
   int V, L, K, M;
   int cols, blocks;    // columns of a block, blocks of a row
+  int table_bits;      // k_penalize_marked: log2 of the places of a block's table
 };
+
+// A logit that occurs c times (the top bit: also among the first `prompt` tokens) and whose first bias is number `first`.
+__device__ __forceinline__ float changed(const PenaltyArgs& a, int b, int v, float x, uint32_t c, int first, float bias_of_first, bool repeated, const float4& p) {
+  if (c) {
+    x = x > 0 ? __fdiv_rn(x, p.x) : __fmul_rn(x, p.x);
+    const uint32_t times = c & 0x7FFFFFFFu;
+    if (times) x = __fsub_rn(__fsub_rn(x, __fmul_rn(p.y, (float)times)), p.z);
+  }
+  if (first != kNoBias) {
+    const int* ids = a.ids + (size_t)b * a.K;
+    const float* bias = a.bias + (size_t)b * a.K;
+    float sum = bias_of_first;
+    if (repeated)
+#pragma unroll 1
+      for (int j = first + 1; j < a.K; ++j)
+        if (ids[j] == v) sum = __fadd_rn(sum, bias[j]);
+    x = __fadd_rn(x, sum);
+  }
+  return x;
+}
 
 // A block takes `cols` columns of one row.  They are read, masked and written as they come; meanwhile it goes through the
 // row's tokens: words of shared memory for the columns that occur (and only those) are cleared, then counted up, integer
@@ -28,10 +49,10 @@ struct PenaltyArgs {
 // are read back, changed and written again.  (Done for every element of a vector in turn instead, the code is so long that
 // a block waits for instructions: 256 rows of 131072 bf16 logits and 4096 tokens 151 us.)  Bound: reading and writing the
 // logits; the tokens are read once per block, from L2.
-template <class T, int THREADS>
+template <class T, int THREADS, bool MARKS>
 __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_penalize(PenaltyArgs a) {
   constexpr int E = 16 / sizeof(T), kCols = THREADS * kVectors * E;
-  extern __shared__ uint32_t count[];              // [kCols]: later occurrences; the top bit: occurs among the first `prompt` tokens
+  extern __shared__ __align__(16) uint32_t count[];      // [kCols]: later occurrences; the top bit: occurs among the first `prompt` tokens
   uint32_t* touched = count + (a.L > 0 ? kCols : 0);                        // [kCols / 32]
   uint16_t* link = reinterpret_cast<uint16_t*>(touched + kCols / 32);       // [kCols]: the first bias of a column
   uint16_t* list = link + (a.K > 0 ? kCols : 0);                            // the marked columns: no more than L + K, or kCols
@@ -42,10 +63,10 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_penalize(PenaltyArg
   const long long row = (long long)b * a.V;
   const int origin = (int)((row + v0) / E * E - row);
   union Vector { uint4 raw; T x[E]; };
-  follow();
+  cudaGridDependencySynchronize();
+  cudaTriggerProgrammaticLaunchCompletion();       // (only now: k_penalize_marked reads tokens before it waits for this kernel)
   const T* from = static_cast<const T*>(a.logits) + row;
   T* to = static_cast<T*>(a.out) + row;
-  const bool marks = a.L > 0 || a.K > 0;
   const int* tokens = a.tokens + (size_t)b * a.L;
   const int* ids = a.ids + (size_t)b * a.K;
   const uint32_t* mask = a.mask + (size_t)b * a.M;
@@ -59,13 +80,14 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_penalize(PenaltyArg
     bits[k][0] = a.M > 0 && v < v1 ? mask[at >> 5] : ~0u;
     bits[k][1] = a.M > 0 && v < v1 && (at & 31) + E > 32 && (at >> 5) + 1 < a.M ? mask[(at >> 5) + 1] : ~0u;
   }
+  if constexpr (MARKS)
 #pragma unroll
-  for (int k = 0; k < kHeld; ++k) held[k] = k * THREADS + (int)threadIdx.x < a.L ? tokens[k * THREADS + threadIdx.x] : -1;
+    for (int k = 0; k < kHeld; ++k) held[k] = k * THREADS + (int)threadIdx.x < a.L ? tokens[k * THREADS + threadIdx.x] : -1;
   // the warp that goes through the biases has the last of them at hand
   const int bias_lane = (int)threadIdx.x - (THREADS - 32), last_bias = (a.K - 1) / 32 * 32 + bias_lane;
-  const int last_id = a.K > 0 && bias_lane >= 0 && last_bias < a.K ? ids[last_bias] : -1;
+  const int last_id = MARKS && a.K > 0 && bias_lane >= 0 && last_bias < a.K ? ids[last_bias] : -1;
   const uint32_t width = v1 - v0;
-  if (marks) {
+  if constexpr (MARKS) {
     for (int i = threadIdx.x; i < kCols / 32; i += THREADS) touched[i] = 0;
     if (threadIdx.x == 0) listed = repeated = 0;
     bool bad = false;
@@ -104,7 +126,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_penalize(PenaltyArg
         if (v + i >= v0 && v + i < v1) to[v + i] = allowed >> i & 1 ? from[v + i] : least;
     }
   }
-  if (!marks) return;
+  if constexpr (!MARKS) return;
   const float4 p = *reinterpret_cast<const float4*>(a.params + 4 * (size_t)b);
   __syncthreads();
   const int prompt = (int)fminf(fmaxf(p.w, 0.0f), 2147483520.0f);
@@ -144,49 +166,188 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_penalize(PenaltyArg
   for (int i = threadIdx.x; i < n; i += THREADS) {
     const int w = list[i], v = origin + w;
     if (a.M > 0 && !(mask[v >> 5] >> (v & 31) & 1)) continue;
-    float x = widen<T>(to[v]);
-    const uint32_t c = a.L > 0 ? count[w] : 0;
-    if (c) {
-      x = x > 0 ? __fdiv_rn(x, p.x) : __fmul_rn(x, p.x);
-      const uint32_t times = c & 0x7FFFFFFFu;
-      if (times) x = __fsub_rn(__fsub_rn(x, __fmul_rn(p.y, (float)times)), p.z);
-    }
-    const int first = a.K > 0 ? link[w] : kNoBias;
-    if (first != kNoBias) {
-      const float* bias = a.bias + (size_t)b * a.K;
-      float sum = bias[first];
-      if (repeated)
-#pragma unroll 1
-        for (int j = first + 1; j < a.K; ++j)
-          if (ids[j] == v) sum = __fadd_rn(sum, bias[j]);
-      x = __fadd_rn(x, sum);
-    }
-    to[v] = narrow<T>(x);
+    const int bias = a.K > 0 ? link[w] : kNoBias;
+    to[v] = narrow<T>(changed(a, b, v, widen<T>(to[v]), a.L > 0 ? count[w] : 0, bias, bias != kNoBias ? a.bias[(size_t)b * a.K + bias] : 0.0f, repeated, p));
   }
 }
 
-template <class T, int THREADS>
-int launch(const ClusterLaunch& L) {
-  constexpr int E = 16 / sizeof(T), kCols = THREADS * kVectors * E;
-  const int B = (int)L.op.shape[0], V = (int)L.op.shape[1];
-  PenaltyArgs a{report_of(L), slot(L, 0).ptr, slot_ptr<int>(L, 1), slot_ptr<float>(L, 2), slot_ptr<int>(L, 3), slot_ptr<float>(L, 4),
-                slot_ptr<uint32_t>(L, 5), result_ptr<void>(L),
-                V, slot(L, 1).C, slot(L, 3).C, slot(L, 5).C, V % E == 0 ? kCols : kCols - E, 0};
-  a.blocks = (V + a.cols - 1) / a.cols;
-  const size_t shared = a.L + a.K == 0 ? 0 : (size_t)kCols * ((a.L > 0 ? 4 : 0) + (a.K > 0 ? 2 : 0)) + kCols / 8 + 2 * std::min<size_t>((size_t)a.L + a.K, kCols);
-  static std::atomic<uint64_t> allowed{0};
-  const int rc = allow_shared(k_penalize<T, THREADS>, (size_t)kCols * 8 + kCols / 8, allowed);
-  if (rc != ACC_OK) return rc;
-  return launch_following(k_penalize<T, THREADS>, dim3((unsigned)B * (unsigned)a.blocks), THREADS, shared, L.stream, a);
+// Large batches: the rows are copied and masked by k_penalize without tokens, at the rate of a copy, and this kernel changes
+// the columns that occur, behind it.  A block takes a range of the columns of one row (all of them, if rows are many), and
+// counts the row's tokens that lie there in a hash table of at least half as many places again as tokens and biases:
+// shared memory goes by the tokens, not by the columns.  It does that before it waits for the copy; then it goes through the
+// table.  Which place a column gets depends on the order of the threads, what is written to it does not.
+constexpr int kMarkedThreads = 512, kMaxTableBits = 14, kMaxTableBytes = (10 << kMaxTableBits) + (4 << kMaxTableBits) / 3;
+constexpr int kEmptyPlace = -1;
+template <class T>
+__global__ void __launch_bounds__(kMarkedThreads, 2) k_penalize_marked(PenaltyArgs a) {
+  extern __shared__ __align__(16) uint32_t count[];                         // [places]
+  const int places = 1 << a.table_bits;
+  int* key = reinterpret_cast<int*>(count + places);                        // [places]: the column
+  uint16_t* link = reinterpret_cast<uint16_t*>(key + places);               // [places]: the first bias of a column
+  uint16_t* list = link + (a.K > 0 ? places : 0);                           // the places that were taken: no more than L + K
+  __shared__ int listed, repeated;
+  const int b = blockIdx.x / a.blocks;
+  const int v0 = (blockIdx.x - b * a.blocks) * a.cols, v1 = min(v0 + a.cols, a.V);
+  const uint32_t width = v1 - v0;
+  const int* tokens = a.tokens + (size_t)b * a.L;
+  const int* ids = a.ids + (size_t)b * a.K;
+  const uint32_t* mask = a.mask + (size_t)b * a.M;
+  int held[kHeld];
+#pragma unroll
+  for (int k = 0; k < kHeld; ++k) held[k] = k * kMarkedThreads + (int)threadIdx.x < a.L ? tokens[k * kMarkedThreads + threadIdx.x] : -1;
+  const int bias_lane = (int)threadIdx.x - (kMarkedThreads - 32), last_bias = (a.K - 1) / 32 * 32 + bias_lane;
+  int id = a.K > 0 && bias_lane >= 0 && last_bias < a.K ? ids[last_bias] : -1;
+  const float4 p = *reinterpret_cast<const float4*>(a.params + 4 * (size_t)b);
+  // (64 places at least: every array is a multiple of 16 bytes)
+  for (int i = threadIdx.x; i < places / 4; i += kMarkedThreads) {
+    reinterpret_cast<uint4*>(count)[i] = make_uint4(0, 0, 0, 0);
+    reinterpret_cast<int4*>(key)[i] = make_int4(kEmptyPlace, kEmptyPlace, kEmptyPlace, kEmptyPlace);
+  }
+  if (a.K > 0)
+    for (int i = threadIdx.x; i < places / 8; i += kMarkedThreads) reinterpret_cast<uint4*>(link)[i] = make_uint4(~0u, ~0u, ~0u, ~0u);
+  if (threadIdx.x == 0) listed = repeated = 0;
+  __syncthreads();
+  const int prompt = (int)fminf(fmaxf(p.w, 0.0f), 2147483520.0f);
+  bool bad = false;
+  const auto place_of = [&](int v, bool& taken) {  // (the table is never full: every probe ends)
+    uint32_t i = (uint32_t)v * 2654435769u >> (32 - a.table_bits);
+    for (;; i = (i + 1) & (places - 1)) {
+      int found = key[i];
+      if (found == kEmptyPlace) {
+        found = atomicCAS(key + i, kEmptyPlace, v);
+        taken = found == kEmptyPlace;
+      }
+      if (taken || found == v) return i;
+    }
+  };
+  const auto put_on_list = [&](bool taken, uint32_t place) {      // by a whole warp, one addition for all of it
+    const uint32_t all = __ballot_sync(~0u, taken);
+    if (all == 0) return;
+    const int lane = threadIdx.x & 31;
+    int first = lane == 0 ? atomicAdd(&listed, __popc(all)) : 0;
+    first = __shfl_sync(~0u, first, 0);
+    if (taken) list[first + __popc(all & ((1u << lane) - 1))] = (uint16_t)place;
+  };
+  const auto note = [&](int v, int i) {
+    bad = bad || v >= a.V;
+    bool taken = false;
+    uint32_t place = 0;
+    if ((uint32_t)(v - v0) < width) {
+      place = place_of(v, taken);
+      if (i >= prompt) atomicAdd(count + place, 1u);
+      else atomicOr(count + place, 0x80000000u);
+    }
+    put_on_list(taken, place);
+  };
+#pragma unroll
+  for (int k = 0; k < kHeld; ++k)
+    if (k * kMarkedThreads < a.L) note(held[k], k * kMarkedThreads + threadIdx.x);
+#pragma unroll 1
+  for (int i0 = kHeld * kMarkedThreads; i0 < a.L; i0 += kMarkedThreads) {
+    const int i = i0 + threadIdx.x;
+    note(i < a.L ? tokens[i] : -1, i);
+  }
+  if (bias_lane >= 0 && a.K > 0) {                 // from the last bias to the first, 32 at a time
+    const int lane = bias_lane;
+    for (int k = last_bias; k >= lane; k -= 32) {
+      const int before = k >= 32 + lane ? ids[k - 32] : -1;
+      bad = bad || id >= a.V;
+      const bool mine = (uint32_t)(id - v0) < width;
+      const uint32_t same = __match_any_sync(~0u, mine ? id : -1 - lane);
+      bool taken = false;
+      const uint32_t place = mine ? place_of(id, taken) : 0;
+      put_on_list(taken, place);
+      __syncwarp();
+      if (mine && ((same & (same - 1)) || link[place] != kNoBias)) repeated = 1;
+      __syncwarp();
+      if (mine && lane == __ffs(same) - 1) link[place] = (uint16_t)k;
+      __syncwarp();
+      id = before;
+    }
+  }
+  if (bad) raise_index(a.report);
+  __syncthreads();
+  cudaTriggerProgrammaticLaunchCompletion();
+  cudaGridDependencySynchronize();
+  T* to = static_cast<T*>(a.out) + (long long)b * a.V;
+  const int n = listed;
+  constexpr int kAhead = 4;
+#pragma unroll 1
+  for (int i0 = threadIdx.x; i0 < n; i0 += kAhead * kMarkedThreads) {
+    int v[kAhead], first[kAhead];
+    float x[kAhead], bias[kAhead];
+    uint32_t c[kAhead], word[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      const int i = i0 + k * kMarkedThreads, place = i < n ? list[i] : 0;
+      v[k] = i < n ? key[place] : kEmptyPlace;
+      x[k] = v[k] >= 0 ? widen<T>(to[v[k]]) : 0.0f;
+      word[k] = v[k] < 0 ? 0 : a.M > 0 ? mask[v[k] >> 5] : ~0u;
+      c[k] = count[place];
+      first[k] = a.K > 0 ? link[place] : kNoBias;
+      bias[k] = first[k] != kNoBias ? a.bias[(size_t)b * a.K + first[k]] : 0.0f;
+    }
+#pragma unroll 1
+    for (int k = 0; k < kAhead; ++k) {
+      if (word[0] >> (v[0] & 31) & 1) to[v[0]] = narrow<T>(changed(a, b, v[0], x[0], c[0], first[0], bias[0], repeated, p));
+#pragma unroll
+      for (int u = 0; u + 1 < kAhead; ++u) v[u] = v[u + 1], x[u] = x[u + 1], c[u] = c[u + 1], word[u] = word[u + 1], first[u] = first[u + 1], bias[u] = bias[u + 1];
+    }
+  }
 }
 
-// Large blocks where they still leave each SM a few: a row's tokens are then gone through fewer times.
+PenaltyArgs arguments(const ClusterLaunch& L) {
+  return {report_of(L), slot(L, 0).ptr, slot_ptr<int>(L, 1), slot_ptr<float>(L, 2), slot_ptr<int>(L, 3), slot_ptr<float>(L, 4),
+          slot_ptr<uint32_t>(L, 5), result_ptr<void>(L), (int)L.op.shape[1], slot(L, 1).C, slot(L, 3).C, slot(L, 5).C, 0, 0, 0};
+}
+
+template <class T, int THREADS, bool MARKS>
+int launch(const ClusterLaunch& L, PenaltyArgs a) {
+  constexpr int E = 16 / sizeof(T), kCols = THREADS * kVectors * E;
+  a.cols = a.V % E == 0 ? kCols : kCols - E;
+  a.blocks = (a.V + a.cols - 1) / a.cols;
+  const size_t shared = !MARKS ? 0 : (size_t)kCols * ((a.L > 0 ? 4 : 0) + (a.K > 0 ? 2 : 0)) + kCols / 8 + 2 * std::min<size_t>((size_t)a.L + a.K, kCols);
+  if (MARKS) {
+    static std::atomic<uint64_t> allowed{0};
+    const int rc = allow_shared(k_penalize<T, THREADS, MARKS>, (size_t)kCols * 8 + kCols / 8, allowed);
+    if (rc != ACC_OK) return rc;
+  }
+  return launch_following(k_penalize<T, THREADS, MARKS>, dim3((unsigned)L.op.shape[0] * (unsigned)a.blocks), THREADS, shared, L.stream, a);
+}
+
+template <class T>
+int launch_marked(const ClusterLaunch& L, PenaltyArgs a) {
+  a.table_bits = 6;
+  while ((2ll << a.table_bits) < 3ll * (a.L + a.K)) ++a.table_bits;
+  // two blocks to an SM, none with fewer than 4096 columns
+  const int B = (int)L.op.shape[0];
+  a.blocks = std::max(1, std::min(2 * sm_count() / B, a.V / 4096));
+  a.cols = (a.V + a.blocks - 1) / a.blocks;
+  const auto bytes = [&](int bits) { return ((size_t)(a.K > 0 ? 10 : 8) << bits) + 2 * ((size_t)a.L + a.K); };
+  static std::atomic<uint64_t> allowed{0};
+  const int rc = allow_shared(k_penalize_marked<T>, (size_t)kMaxTableBytes, allowed);
+  if (rc != ACC_OK) return rc;
+  ++L.extra_launches;
+  return launch_following(k_penalize_marked<T>, dim3((unsigned)B * (unsigned)a.blocks), kMarkedThreads, bytes(a.table_bits), L.stream, a);
+}
+
+// From this many logits on, two kernels (rows of 131072 with a mask; one kernel, two): 256 of bf16 with 4096 tokens 57, 48 us,
+// with 256 tokens 43, 28; 20 of fp32 with 6000 tokens 29, 30; 8 of bf16 with 6000 23, 26.
+constexpr int64_t kTwoKernels = 1 << 22;
 template <class T>
 int launch(const ClusterLaunch& L) {
   if (L.op.shape[0] == 0 || L.op.shape[1] == 0) return ACC_OK;
+  PenaltyArgs a = arguments(L);
+  const int64_t marks = (int64_t)a.L + a.K;
+  if (marks == 0) return launch<T, 256, false>(L, a);
+  if (L.op.shape[0] * L.op.shape[1] >= kTwoKernels && 3 * marks <= 2 << kMaxTableBits) {
+    const int rc = launch<T, 256, false>(L, a);
+    return rc == ACC_OK ? launch_marked<T>(L, a) : rc;
+  }
+  // large blocks where they still leave each SM a few: a row's tokens are then gone through fewer times
   constexpr int64_t kLarge = 512 * kVectors * (16 / sizeof(T));
   const int64_t blocks = L.op.shape[0] * ((L.op.shape[1] + kLarge - 1) / kLarge);
-  return blocks >= 4 * sm_count() ? launch<T, 512>(L) : launch<T, 256>(L);
+  return blocks >= 4 * sm_count() ? launch<T, 512, true>(L, a) : launch<T, 256, true>(L, a);
 }
 
 int launch_penalize(const ClusterLaunch& L) {

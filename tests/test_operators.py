@@ -700,7 +700,8 @@ def _check_penalties(prog, d, got, dtype, strict=True):
 @pytest.mark.parametrize("dtype", REAL)
 @pytest.mark.parametrize("B_,V,Lh,K,masked", [(1, 1, 3, 1, True), (3, 7, 20, 9, True), (2, 33, 0, 0, True), (5, 32, 1, 0, False), (2, 4096, 500, 0, True),
                                               (2, 4097, 300, 40, True), (3, 8191, 0, 70, False), (2, 8197, 1000, 3, True), (1, 50001, 9000, 300, True),
-                                              (2, 24576, 0, 0, False), (4, 0, 3, 2, False)])
+                                              (2, 24576, 0, 0, False), (4, 0, 3, 2, False), (50, 90001, 40, 3, True), (64, 70000, 5000, 0, False),
+                                              (300, 16384, 0, 40, True), (43, 100000, 10920, 2, True), (43, 100000, 10921, 2, False)])
 def test_penalties(B_, V, Lh, K, masked, dtype):
     if V == 0:
         d = {"logits": to_type(np.zeros((B_, 0)), dtype), "tokens": np.full((B_, Lh), -1, np.int32), "params": np.ones((B_, 4), np.float32),
@@ -713,15 +714,18 @@ def test_penalties(B_, V, Lh, K, masked, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("rows", [3, 4500])
 @pytest.mark.parametrize("dtype", REAL)
-def test_penalties_of_infinities_and_repeated_biases(dtype):
+def test_penalties_of_infinities_and_repeated_biases(dtype, rows):
     d = _penalty_inputs(np.random.default_rng(2), 3, 1001, 50, 200, True, dtype)
     logits = O.widen(d["logits"], dtype)
     logits[0, ::5], logits[1, ::7], logits[2, ::3] = -np.inf, np.inf, np.nan
     d["logits"] = to_type(logits, dtype)
     d["bias_ids"][:, ::3] = 17                               # many biases of one column
     d["bias_ids"][1, :] = 1000
-    prog = W.penalized_logits(3, 1001, 50, 200, True, dtype)
+    if rows > 3:                                             # so many rows that they are copied by one kernel and changed by another
+        d = {k: np.tile(v, (rows // 3, 1)) for k, v in d.items()}
+    prog = W.penalized_logits(rows, 1001, 50, 200, True, dtype)
     first = gpu(prog, d)["penalized"]
     _check_penalties(prog, d, first, dtype)
     assert np.array_equal(first.view(np.uint8), gpu(prog, d)["penalized"].view(np.uint8))
@@ -729,13 +733,14 @@ def test_penalties_of_infinities_and_repeated_biases(dtype):
 
 @pytest.mark.gpu
 def test_penalties_report_numbers_outside_their_range():
-    d = _penalty_inputs(np.random.default_rng(4), 2, 500, 30, 4, False, "f32")
-    prog = W.penalized_logits(2, 500, 30, 4, False)
-    for name in ("tokens", "bias_ids"):
-        bad = {k: v.copy() for k, v in d.items()}
-        bad[name][1, 2] = 500
-        bad[name][1, 3] = 2 ** 31 - 1
-        _check_penalties(prog, bad, gpu(prog, bad, reported=True)["penalized"], "f32", strict=False)
+    for rows, V in ((2, 500), (50, 90000)):
+        d = _penalty_inputs(np.random.default_rng(4), rows, V, 30, 4, False, "f32")
+        prog = W.penalized_logits(rows, V, 30, 4, False)
+        for name in ("tokens", "bias_ids"):
+            bad = {k: v.copy() for k, v in d.items()}
+            bad[name][1, 2] = V
+            bad[name][1, 3] = 2 ** 31 - 1
+            _check_penalties(prog, bad, gpu(prog, bad, reported=True)["penalized"], "f32", strict=False)
 
 
 @pytest.mark.gpu

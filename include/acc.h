@@ -240,7 +240,9 @@ int acc_edges(const acc_graph* g, int32_t* F, int32_t* nF, int32_t* I, int32_t* 
  *     D = iparam[1] is a multiple of 8 up to 256, Hq a multiple of Hk.
  *     scale = fparam[0].  iparam[2] > 0: only the last iparam[2] tokens (a sliding
  *     window).  A request without tokens yields zeros.  One element type of F32,
- *     F16, BF16; products, softmax and sums are held in 32 bits.  Reported: a
+ *     F16, BF16; products, softmax and sums are held in 32 bits.  What a request
+ *     does not attend to may hold anything.  An infinite value that it does attend
+ *     to makes its element of the result infinite or not a number.  Reported: a
  *     negative length (no tokens), a length beyond W * block (cut off), a block
  *     outside the cache (its tokens are left out).
  * PENALIZE {logits[B, V], tokens[B, L], params[B, 4], bias_ids[B, K], bias[B, K], mask[B, M]} -> [B, V]

@@ -139,7 +139,7 @@ __device__ Cursor<TILE> find_place(const AttentionArgs& a, Place* shared, long l
   if (any && upto - mine <= start && start < upto) {
     long long at = upto - mine;
     int r = r0;
-    for (;; ++r) {
+    for (; r + 1 < r1; ++r) {
       const long long n = (long long)tiles_of<TILE>(span_of(a, r)) * a.units;
       if (at + n > start) break;
       at += n;
@@ -973,9 +973,10 @@ int run(const ClusterLaunch& L, K kernel, std::atomic<uint64_t>& allowed) {
 }
 
 // Calls f(type, DP, shape, kernel) for the kernel that a launch takes: heads padded to 64, 96, 128 or 256 elements; for
-// 16-bit types sixteen heads at a time where a key head has more than eight (beyond 128 elements the registers do not hold
-// them), and the four warps on four key heads where there are so many: their rows lie side by side, so that what is read
-// together is four times as long.
+// 16-bit types sixteen heads at a time where a key head has more than eight; and the four warps on four key heads where
+// there are many requests: their rows lie side by side, so that what is read together is four times as long (2 GB of keys
+// and values of 20 heads of 80: 443 us with four warps on one head, 302 so; of 8 heads of 128 no difference).  With few
+// requests it would leave more records to join: one of 8000 tokens 21 us, so 30.
 constexpr int kManyHeads = 128;
 template <class T, int DP, int NT, class F>
 auto choose_ways(const ClusterLaunch& L, F f) {
@@ -991,7 +992,7 @@ auto choose_half(const ClusterLaunch& L, F f) {
   if (D <= 64) return wide ? choose_ways<T, 64, 2>(L, f) : choose_ways<T, 64, 1>(L, f);
   if (D <= 96) return wide ? choose_ways<T, 96, 2>(L, f) : choose_ways<T, 96, 1>(L, f);
   if (D <= 128) return wide ? choose_ways<T, 128, 2>(L, f) : choose_ways<T, 128, 1>(L, f);
-  return choose_ways<T, 256, 1>(L, f);
+  return wide ? choose_ways<T, 256, 2>(L, f) : choose_ways<T, 256, 1>(L, f);
 }
 template <class F>
 auto choose(const ClusterLaunch& L, F f) {

@@ -339,6 +339,16 @@ def test_what_is_overwritten_is_not_read_later():
         assert _schedule_status(p, where, B.UNFUSED) == ("ACC_ERR_ILLEGAL_SCATTER" if behind else "ACC_OK")
 
 
+def test_generated_source_matches_the_program(capsys):
+    """The combinators around the operators of a decode step: what the generator prints today."""
+    import os
+    import re
+    from paper_2407_13585_b200 import build, instantiate
+    text = open(os.path.join(build.CSRC, "programs", "prog_decode_step.cu")).read()
+    instantiate.main(re.match(r"// Generated by `python -m paper_2407_13585_b200.instantiate (.*)`\.", text).group(1).split())
+    assert capsys.readouterr().out == text
+
+
 def test_binding_asks_for_the_node_s_element_size():
     import torch
     prog = W.append_rows(32, 16, 3)
@@ -553,6 +563,16 @@ ATTENTION = [
     (20, 4, 200, 10, 33, [2, 40, 400]),
     (2, 2, 24, 100, 0, [1000, 0, 0, 0, 0]),
     (12, 12, 16, 3, 0, list(range(0, 40))),
+    (32, 2, 256, 16, 0, [300, 45, 1]),
+    (34, 2, 64, 16, 0, [100, 130]),
+    (71, 1, 72, 16, 0, [222]),
+    # so many requests that the warps of a block take a key head each
+    (12, 4, 80, 16, 0, [(37 * i) % 211 for i in range(40)]),
+    (4, 4, 256, 8, 50, [(37 * i) % 111 for i in range(33)]),
+    (80, 8, 64, 16, 0, [(53 * i) % 150 for i in range(20)]),
+    (48, 4, 112, 20, 0, [(29 * i) % 90 for i in range(34)]),
+    (8, 8, 128, 16, 0, [(41 * i) % 400 for i in range(16)]),
+    (64, 4, 200, 16, 0, [70] * 32),
 ]
 
 
@@ -630,6 +650,33 @@ def test_paged_attention_of_infinities():
     want = oracle(prog, d).exact[5]
     assert np.isnan(want[1:]).all() and np.isnan(got[1:]).all()
     assert np.all(np.abs(got[0] - want[0]) <= 1e-5) and np.isfinite(got[0]).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", REAL)
+def test_paged_attention_to_infinite_values(dtype):
+    d = _attention_inputs(np.random.default_rng(6), 2, 2, 1, 64, 8, [30, 200], dtype)
+    prog = W.paged_attention(2, 2, 1, 64, d["keys"].shape[0], 8, d["table"].shape[1], dtype, 0.1)
+    at = lambda b, p: d["table"][b, p // 8] * 8 + p % 8
+    values = O.widen(d["values"], dtype)
+    values[at(0, 3), 5], values[at(1, 180), 7] = np.inf, -np.inf
+    d["values"] = to_type(values, dtype)
+    got = O.widen(gpu(prog, d)["out"], dtype).reshape(2, 2, 64)
+    hit = np.zeros((2, 2, 64), bool)
+    hit[0, :, 5] = hit[1, :, 7] = True
+    assert not np.isfinite(got[hit]).any() and np.isfinite(got[~hit]).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", REAL)
+def test_paged_attention_of_many_requests_split_over_blocks(dtype):
+    """Four key heads to a block, and requests of very different lengths: units that many blocks share beside whole ones."""
+    lens = [3000 if i % 50 == 7 else (i * 7) % 60 for i in range(150)]
+    d = _attention_inputs(np.random.default_rng(12), len(lens), 4, 4, 64, 16, lens, dtype)
+    prog = W.paged_attention(len(lens), 4, 4, 64, d["keys"].shape[0], 16, d["table"].shape[1], dtype, 0.125)
+    first = gpu(prog, d)["out"]
+    _check_attention(prog, d, first, dtype)
+    assert np.array_equal(first.view(np.uint8), gpu(prog, d)["out"].view(np.uint8))
 
 
 @pytest.mark.gpu
@@ -826,6 +873,62 @@ def test_decode_steps_on_another_stream_and_replayed():
         torch.cuda.synchronize()
         b.g.finish()
         _check_step(prog, data, b.outputs(), "bf16")
+
+
+@pytest.mark.gpu
+def test_a_captured_step_behind_work_of_two_streams():
+    """Captured with a fork and a join before and behind the run: what the run reads comes from the other stream."""
+    import torch
+    prog, d = _step_inputs(np.random.default_rng(3), dtype="f16")
+    b = Bound(prog, d)
+    b.g.run(B.FUSED)
+    fresh = {n: b.t[n].clone() for n in ("tokens", "k", "old", "q")}
+    late = {n: torch.zeros_like(t) for n, t in fresh.items()}
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    results = [prog.nodes[o].name for o in prog.outputs]
+    copies = {}
+    with torch.cuda.graph(graph):
+        main = torch.cuda.current_stream()
+        side.wait_stream(main)
+        with torch.cuda.stream(side):
+            for n in fresh:
+                b.t[n].copy_(late[n])
+        main.wait_stream(side)
+        b.g.run(B.FUSED, finish=False)
+        side.wait_stream(main)
+        with torch.cuda.stream(side):
+            for n in results:
+                copies[n] = b.t[n].clone()
+        main.wait_stream(side)
+    for n in fresh:
+        late[n].copy_(fresh[n])
+        b.t[n].zero_()
+    for n in results:
+        b.t[n].zero_()
+    graph.replay()
+    torch.cuda.synchronize()
+    b.g.finish()
+    _check_step(prog, d, {prog.nodes[o].name: from_cuda(copies[prog.nodes[o].name], prog.nodes[o].dtype) for o in prog.outputs}, "f16")
+
+
+@pytest.mark.gpu
+def test_two_handles_in_flight_on_two_streams():
+    """Each with a workspace of its own, run again and again at the same time."""
+    import torch
+    steps = [_step_inputs(np.random.default_rng(20 + k), dtype=dt) for k, dt in enumerate(("bf16", "f32"))]
+    bound = [Bound(prog, d) for prog, d in steps]
+    streams = [torch.cuda.Stream() for _ in steps]
+    for b in bound:
+        b.g.ensure_workspace(B.FUSED)
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for b, s in zip(bound, streams):
+            with torch.cuda.stream(s):
+                b.g.run(B.FUSED, finish=False)
+    for (prog, d), b, s, dt in zip(steps, bound, streams, ("bf16", "f32")):
+        with torch.cuda.stream(s):
+            b.g.finish()
+        _check_step(prog, d, b.outputs(), dt)
 
 
 @pytest.mark.gpu

@@ -961,14 +961,15 @@ int run(const ClusterLaunch& L, K kernel, std::atomic<uint64_t>& allowed) {
   }
   const int rc = allow_shared(kernel, S::kShared, allowed);
   if (rc != ACC_OK) return rc;
-  a.join_rows = (long long)a.B * a.units * kManyRecords < grid ? 1 : std::min(8, S::kRows * S::kWays);
+  const int heads = S::kRows * S::kWays, pieces = DP / kPiece;
+  a.join_rows = joins_of(a) * heads * pieces <= 2 * sm_count() ? 1 : std::min(8, heads);
   // (not launched early: beside the kernel before it an SM is divided for less shared memory, and keeps to that while the
   // blocks that did fit run; 31 windows of 4096 tokens, back to back: 101 us, launched early 154)
   kernel<<<grid, kThreads, S::kShared, L.stream>>>(a);
   const int first = launched();
   if (first != ACC_OK || !splits) return first;
   ++L.extra_launches;
-  return launch_following(k_join<T, DP, S::kRows, S::kWays>, dim3((unsigned)joins_of(a), S::kRows * S::kWays / a.join_rows, a.join_rows == 1 ? DP / kPiece : 1),
+  return launch_following(k_join<T, DP, S::kRows, S::kWays>, dim3((unsigned)joins_of(a), heads / a.join_rows, a.join_rows == 1 ? pieces : 1),
                           kJoinThreads, 0, L.stream, a);
 }
 

@@ -233,7 +233,9 @@ int acc_edges(const acc_graph* g, int32_t* F, int32_t* nF, int32_t* I, int32_t* 
  *     type, any of the five.  As for PERMUTE, every other use of dest must come in
  *     an earlier cluster, because the result may be bound to dest's own buffer:
  *     then only the rows that are put are touched; bound elsewhere, dest is copied
- *     first.  Reported: a slot beyond S (the row is left out).
+ *     first.  Two of them in a row, for one `slots` and arrays of one shape and type
+ *     (keys and values), share a launch.  Reported: a slot beyond S (the row is left
+ *     out).
  * PAGED_ATTENTION {q[B, Hq * D], keys[S, Hk * D], values[S, Hk * D], table[B, W], lens[B]} -> [B, Hq * D]
  *     Row b attends to the tokens of request b: for head h, with K and V those of
  *     head h / (Hq / Hk), the mean of V weighted with softmax(scale * q . K).

@@ -162,6 +162,24 @@ static int check_operator_buffers(const Graph& g, const std::vector<int32_t>& pi
   return ACC_OK;
 }
 
+// Whether node b, in the cluster behind a's, may be computed at the same time as a by the same launch: both put rows at the
+// same slots into arrays of one shape and type (keys and values), and neither writes what the other reads or writes.
+static bool may_run_together(const Graph& g, int a, int b) {
+  const acc_node_desc &x = g.nodes[a].d, &y = g.nodes[b].d;
+  if (x.kind != ACC_PUT_ROWS || y.kind != ACC_PUT_ROWS || x.inputs[1] != y.inputs[1] || x.dtype != y.dtype || x.shape[0] != y.shape[0] || x.shape[1] != y.shape[1])
+    return false;
+  const auto apart = [&](int i, int j) {                    // (arrays in the workspace have places of their own)
+    const Node &m = g.nodes[i], &n = g.nodes[j];
+    if (i == j) return false;
+    if (!m.dev || !n.dev) return true;
+    const uintptr_t p = reinterpret_cast<uintptr_t>(m.dev), q = reinterpret_cast<uintptr_t>(n.dev);
+    return p + array_bytes(m) <= q || q + array_bytes(n) <= p;
+  };
+  for (int s = 0; s < 3; ++s)
+    if (!apart(a, y.inputs[s]) || !apart(b, x.inputs[s])) return false;
+  return apart(a, b);
+}
+
 int build_schedule(Graph& g, int executor, Schedule& sch) {
   const int n = (int)g.nodes.size();
   sch = Schedule{};
@@ -233,6 +251,9 @@ int build_schedule(Graph& g, int executor, Schedule& sch) {
     ctrl += align_up((size_t)sb, 256);
     sch.steps.push_back(st);
   }
+  for (size_t k = 0; k + 1 < sch.steps.size(); ++k)
+    if ((k == 0 || !sch.steps[k - 1].together_with_next) && may_run_together(g, sch.steps[k].first_node, sch.steps[k + 1].first_node))
+      sch.steps[k].together_with_next = true;
   sch.ctrl_bytes = ctrl;
   sch.to_clear.clear();
   for (const ClusterStep& st : sch.steps) {
@@ -411,16 +432,19 @@ int run_schedule(Graph& handle, Graph& g, Schedule& sch, void* workspace, size_t
   g.launches = 0;
   g.schedule = sch.text;
   if (!mark(marks, stream)) return set_error(ACC_ERR_CUDA, "recording an event failed: %s", cudaGetErrorString(cudaGetLastError()));
-  for (ClusterStep& st : sch.steps) {
+  for (size_t k = 0; k < sch.steps.size(); ++k) {
+    ClusterStep& st = sch.steps[k];
     st.launch.stream = stream;
     st.launch.spin_limit = g.spin_limit;
     st.launch.status = report.words.get();
     st.launch.run_id = report.run_id;
     st.launch.extra_launches = 0;
-    const int rc = st.kernel->launch(st.launch);
+    const bool launched = k > 0 && sch.steps[k - 1].together_with_next;
+    st.launch.also = st.together_with_next ? &sch.steps[k + 1].launch : nullptr;
+    const int rc = launched ? ACC_OK : st.kernel->launch(st.launch);
     if (rc != ACC_OK) return rc;
     if (!mark(marks, stream)) return set_error(ACC_ERR_CUDA, "recording an event failed: %s", cudaGetErrorString(cudaGetLastError()));
-    g.launches += st.kernel->passes + st.launch.extra_launches;
+    if (!launched) g.launches += st.kernel->passes + st.launch.extra_launches;
   }
   return ACC_OK;
 }

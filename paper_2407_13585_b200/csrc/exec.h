@@ -19,6 +19,7 @@ struct ClusterStep {
   const KernelEntry* kernel = nullptr;
   ClusterLaunch launch;
   size_t scratch_off = 0, scratch_bytes = 0, zero_bytes = 0;
+  bool together_with_next = false;   // one launch for this cluster and the next one: rows put into two arrays at the same slots
 };
 
 struct Schedule {

@@ -333,7 +333,6 @@ __global__ void __launch_bounds__(kJoinThreads) k_join(AttentionArgs a) {
 }
 
 __device__ __forceinline__ uint32_t shared_address(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-__device__ __forceinline__ void copy16(uint32_t to, const void* from) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory"); }
 // 16 bytes to shared memory, or 16 zeros
 __device__ __forceinline__ void copy16(uint32_t to, const void* from, bool there) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(there ? 16 : 0) : "memory");
@@ -372,7 +371,7 @@ __device__ __forceinline__ uint32_t ask_for(const AttentionArgs& a, const Cursor
   // in chunks: an array of 2^31 elements has fewer than 2^30
   const uint32_t offset = there ? (uint32_t)((slot * a.Hk + kv) * a.D / PER) : 0;
   const uint4 *keys = static_cast<const uint4*>(a.keys), *values = static_cast<const uint4*>(a.values);
-  const bool whole = a.D == DP && have == (TOKENS == 32 ? ~0u : (1u << TOKENS) - 1);
+  const bool all = have == (TOKENS == 32 ? ~0u : (1u << TOKENS) - 1);
 #pragma unroll
   for (int r = 0; r < TOKENS; r += ROWS) {
     const int row = r + lane / ACROSS;
@@ -382,11 +381,13 @@ __device__ __forceinline__ uint32_t ask_for(const AttentionArgs& a, const Cursor
       const int chunk = k + lane % ACROSS;
       const uint32_t k_at = stage + (row * CHUNKS + (chunk ^ sk(row))) * 16, v_at = stage + ((TOKENS + row) * CHUNKS + (chunk ^ sv(row))) * 16;
       if (CHUNKS > DP / PER && chunk >= DP / PER) continue;
-      if (whole) {
-        copy16(k_at, keys + (from + chunk));
-        copy16(v_at, values + (from + chunk));
+      const bool inside = chunk * PER < a.D;               // (the same for every row: a lane's chunk)
+      if (all) {
+        const uint32_t at = from + (inside ? chunk : 0);
+        copy16(k_at, keys + at, inside);
+        copy16(v_at, values + at, inside);
       } else {
-        const bool want = (have >> row & 1) && chunk * PER < a.D;
+        const bool want = (have >> row & 1) && inside;
         const uint32_t at = want ? from + chunk : 0;
         copy16(k_at, keys + at, want);
         copy16(v_at, values + at, want);

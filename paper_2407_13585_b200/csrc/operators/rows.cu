@@ -11,8 +11,8 @@ namespace {
 struct RowArgs {
   Report report;
   const int* slots;
-  const void* rows;
-  void* out;
+  const void* rows[2];  // of one array, or of two of one shape (the grid's second dimension)
+  void* out[2];
   int* owner;          // the last row of every slot that a row is put into; null: the rows look for a later one themselves
   int T, S, units;     // units of the vector type per row
   int pieces;          // warps per row
@@ -45,7 +45,7 @@ __global__ void __launch_bounds__(128) k_put_rows(RowArgs a) {
     return;
   }
   const int first = piece * 32 * kUnitsPerLane + lane;
-  const U* from = static_cast<const U*>(a.rows) + (size_t)t * a.units;
+  const U* from = static_cast<const U*>(a.rows[blockIdx.y]) + (size_t)t * a.units;
   U v[kUnitsPerLane];
 #pragma unroll
   for (int k = 0; k < kUnitsPerLane; ++k)
@@ -60,7 +60,7 @@ __global__ void __launch_bounds__(128) k_put_rows(RowArgs a) {
     later = __any_sync(~0u, later);
   }
   if (later) return;
-  U* to = static_cast<U*>(a.out) + (size_t)at * a.units;
+  U* to = static_cast<U*>(a.out[blockIdx.y]) + (size_t)at * a.units;
 #pragma unroll
   for (int k = 0; k < kUnitsPerLane; ++k)
     if (first + 32 * k < a.units) to[first + 32 * k] = v[k];
@@ -102,16 +102,19 @@ int launch_put_rows(const ClusterLaunch& L) {
   const size_t e = element_bytes(L.op.dtype);
   const size_t row_bytes = (size_t)L.op.shape[1] * e, bytes = row_bytes * L.op.shape[0];
   if (bytes == 0) return ACC_OK;
-  const void* dest = slot(L, 0).ptr;
-  void* out = result_ptr<void>(L);
   int launches = 0, rc = ACC_OK;
-  if (dest != out) {
+  const ClusterLaunch* both[2] = {&L, L.also};
+  for (int k = 0; k < (L.also ? 2 : 1) && rc == ACC_OK; ++k) {
+    const void* dest = slot(*both[k], 0).ptr;
+    void* out = result_ptr<void>(*both[k]);
+    if (dest == out) continue;
     const size_t vectors = bytes / 16;
     const int grid = (int)std::min<size_t>(std::max<size_t>((vectors + 1023) / 1024, 1), (size_t)sm_count() * 8);
     rc = launch_following(k_copy_array, dim3(grid), 256, 0, L.stream, static_cast<const uint4*>(dest), static_cast<uint4*>(out), vectors, bytes);
     ++launches;
   }
-  RowArgs a{report_of(L), slot_ptr<int>(L, 1), slot(L, 2).ptr, out, nullptr, (int)slot(L, 1).C, (int)L.op.shape[0], 0, 1};
+  RowArgs a{report_of(L), slot_ptr<int>(L, 1), {slot(L, 2).ptr, L.also ? slot(*L.also, 2).ptr : nullptr},
+            {result_ptr<void>(L), L.also ? result_ptr<void>(*L.also) : nullptr}, nullptr, (int)slot(L, 1).C, (int)L.op.shape[0], 0, 1};
   if (a.T > 0 && rc == ACC_OK) {
     if (a.T > kRowsThatLook) {
       a.owner = reinterpret_cast<int*>(L.scratch);
@@ -123,7 +126,7 @@ int launch_put_rows(const ClusterLaunch& L) {
     const int unit = row_bytes % 16 == 0 ? 16 : row_bytes % 4 == 0 ? 4 : 2;
     a.units = (int)(row_bytes / unit);
     a.pieces = (a.units + 32 * kUnitsPerLane - 1) / (32 * kUnitsPerLane);
-    const dim3 grid((unsigned)(((long long)a.T * a.pieces + 3) / 4));
+    const dim3 grid((unsigned)(((long long)a.T * a.pieces + 3) / 4), L.also ? 2 : 1);
     if (rc == ACC_OK) rc = launch_following(unit == 16 ? k_put_rows<16> : unit == 4 ? k_put_rows<4> : k_put_rows<2>, grid, 128, 0, L.stream, a);
     ++launches;
   }

@@ -24,6 +24,7 @@ struct ClusterLaunch {
   acc_node_desc op{};
   int slot[kMaxSlots] = {}, result = 0;
   int slot_dtype[kMaxSlots] = {};
+  const ClusterLaunch* also = nullptr;   // a second operator of this kind and these shapes that the launch takes along (exec.h, together_with_next)
   mutable int extra_launches = 0;   // set by a launcher that took more launches than its entry's `passes` (data-dependent paths)
 };
 

@@ -484,6 +484,41 @@ def test_put_rows(S, C, T, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("T", [40, 400])
+def test_rows_put_into_two_arrays_at_once(T):
+    """Keys and values share the launches, unless the one reads what the other writes; the same results either way."""
+    import torch
+    rng = np.random.default_rng(T)
+    S, C = 90, 24
+    d = {n: to_type(rng.normal(size=(S, C)), "bf16") for n in ("keys", "values")} | {n: to_type(rng.normal(size=(T, C)), "bf16") for n in ("k", "v")}
+    d["slots"] = rng.integers(-1, S, T).astype(np.int32)
+    prog = W.append_rows(S, C, T, "bf16")
+    want = oracle(prog, d)
+    for executor in (B.FUSED, B.UNFUSED):
+        for into in (None, {"new_keys": "keys", "new_values": "values"}, {"new_values": "values"}):
+            b = Bound(prog, d, into)
+            b.g.run(executor)
+            got = b.outputs()
+            for o in prog.outputs:
+                assert np.array_equal(got[prog.nodes[o].name], want.values[o])
+            copied = 2 - len(into or ())
+            assert b.g.launch_count() == copied + (1 if T <= 256 else 2)
+            assert len(b.g.run_timed(executor)) == 2
+    # the second array's rows lie where the first one's result goes: one after the other
+    b = Bound(prog, d)
+    room = torch.zeros(max(S, T), C, dtype=torch.bfloat16, device="cuda")
+    b.g.bind(prog.id("new_keys"), room[:S])
+    b.g.bind(prog.id("v"), room[:T])
+    b.g.run(B.FUSED)
+    assert b.g.launch_count() == (4 if T <= 256 else 6)
+    if T <= S:
+        new_keys = want.values[prog.id("new_keys")]
+        assert np.array_equal(from_cuda(room[:S], "bf16"), new_keys)
+        again = oracle(prog, d | {"v": new_keys[:T]})
+        assert np.array_equal(b.outputs()["new_values"], again.values[prog.id("new_values")])
+
+
+@pytest.mark.gpu
 def test_put_rows_reports_slots_beyond_the_array():
     d = {"dest": np.zeros((4, 6), np.float32), "slots": ints(3, 4, 0, 2 ** 31 - 1, -2 ** 31), "rows": np.ones((5, 6), np.float32)}
     prog = _put_program(4, 6, 5, "f32")

@@ -376,7 +376,8 @@ int acc_run(acc_graph* g, void* workspace, size_t workspace_bytes, void* cuda_st
 int acc_finish(acc_graph* g, void* workspace, void* cuda_stream);
 /* acc_run followed by acc_finish, with a CUDA event before the first launch and
  * after every cluster: ms_per_cluster_out[k] receives the device time of the
- * k-th launch in execution order (up to `cap` entries), *n_out their number.
+ * k-th cluster in execution order (up to `cap` entries; next to nothing for one
+ * that shares the launch of the cluster before it), *n_out their number.
  * For looking at where a program's time goes; the events cost a little, so time
  * whole programs with acc_run. */
 int acc_run_timed(acc_graph* g, void* workspace, size_t workspace_bytes, void* cuda_stream, int executor,

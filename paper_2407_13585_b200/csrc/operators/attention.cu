@@ -934,7 +934,7 @@ AttentionArgs arguments(const ClusterLaunch& L) {
 template <class S>
 int grid_of(AttentionArgs& a, bool& splits) {
   a.units = a.Hk / S::kWays * ((a.group + S::kRows - 1) / S::kRows);
-  const long long room = (long long)a.W * a.block.d;
+  const long long room = std::min<long long>((long long)a.W * a.block.d, 0x7FFFFFFF);       // (lengths are 32-bit numbers)
   const long long tiles = std::max<long long>((room + S::kTile - 1) / S::kTile, 1) * a.B * a.units;
   splits = room > S::kTile;
   return a.grid = (int)std::min<long long>(tiles, std::min((long long)sm_count() * S::kResident, (long long)kMaxGrid));

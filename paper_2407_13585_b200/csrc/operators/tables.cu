@@ -64,7 +64,8 @@ __global__ void __launch_bounds__(kThreads) k_block_table(TableArgs a) {
   __shared__ int4 rows[kTableRows + 2];                       // kept, end, from (see table_entry)
   follow();
   const int f0 = blockIdx.x * a.tile, f1 = (int)min((long long)f0 + a.tile, (long long)a.R * a.W);
-  const int r0 = (uint32_t)f0 / a.width, r1 = (uint32_t)(f1 - 1) / a.width + 1;
+  // (rows of no entries: one block that only looks for what there is to report)
+  const int r0 = (uint32_t)f0 / a.width, r1 = a.W == 0 ? a.R : (int)((uint32_t)(f1 - 1) / a.width) + 1;
   const auto length = [&](int row) { return row < r1 ? a.lens[row] : 0; };
   const auto old_length = [&](int row) { return row < r1 && a.old_lens ? a.old_lens[row] : 0; };
   int len = length(r0 + threadIdx.x), old_len = old_length(r0 + threadIdx.x);
@@ -83,7 +84,7 @@ __global__ void __launch_bounds__(kThreads) k_block_table(TableArgs a) {
       const uint32_t start = add_up_to(base, s.before);
       // the list may end inside the row, or before it; from + j < N for all j < end
       const int from = (int)min(start, (uint32_t)a.N) - had;
-      rows[row - r0] = make_int4(min(had, need), (int)min((long long)need, (long long)a.N - from), from, 0);
+      if (a.W > 0) rows[row - r0] = make_int4(min(had, need), (int)min((long long)need, (long long)a.N - from), from, 0);
       if (len < 0 || old_len < 0 || need > a.W || add_up_to(start, taken) > (uint32_t)a.N) raise_index(a.report);
     }
     base = add_up_to(base, s.all);
@@ -121,12 +122,11 @@ int launch_block_table(const ClusterLaunch& L) {
   const bool grow = L.op.n_inputs == 4;
   TableArgs a{report_of(L), slot_ptr<int>(L, 0), slot_ptr<int>(L, 1), grow ? slot_ptr<int>(L, 2) : nullptr, grow ? slot_ptr<int>(L, 3) : nullptr,
               result_ptr<int>(L), t.R, t.C, (int)slot(L, 1).C, 0, divisor((uint32_t)L.op.iparam[0]), divisor((uint32_t)std::max<int64_t>(L.op.shape[1], 1))};
-  if (count == 0) return ACC_OK;
   // two blocks to an SM, if that leaves each at least four elements a thread
   const long long even = (count + 2 * sm_count() - 1) / (2 * sm_count());
   a.tile = (int)std::min<long long>(kTableTile, (even + 4 * kThreads - 1) / (4 * kThreads) * (4 * kThreads));
   a.tile = (int)std::min<int64_t>(a.tile, kTableRows * (int64_t)a.W);
-  return launch_following(k_block_table, dim3((unsigned)((count + a.tile - 1) / a.tile)), kThreads, 0, L.stream, a);
+  return launch_following(k_block_table, dim3((unsigned)std::max<long long>((count + a.tile - 1) / std::max(a.tile, 1), 1)), kThreads, 0, L.stream, a);
 }
 
 struct SlotArgs {

@@ -872,6 +872,56 @@ def _check_step(prog, d, got, dtype):
     assert np.array_equal(got["best"], got["penalized"].max(1))
 
 
+@pytest.mark.gpu
+def test_a_decode_step_with_arrays_in_the_workspace():
+    """Only the attention's result and the largest logits are asked for: tables, slots and caches lie in the workspace."""
+    for dtype in REAL:
+        prog, d = _step_inputs(np.random.default_rng(5), dtype=dtype)
+        want = oracle(prog, d)
+        few = W.Program(prog.name, prog.nodes, [prog.id("out"), prog.id("best")])
+        full = gpu(prog, d)
+        for executor in (B.FUSED, B.UNFUSED):
+            got = gpu(few, d, executor)
+            assert np.array_equal(got["best"], want.values[prog.id("best")])
+            assert np.array_equal(got["out"].view(np.uint8), full["out"].view(np.uint8))
+
+
+@pytest.mark.gpu
+def test_keys_and_values_may_be_one_array():
+    rng = np.random.default_rng(13)
+    d = _attention_inputs(rng, 3, 4, 2, 64, 16, [5, 100, 33], "bf16")
+    d["values"] = d["keys"]
+    two = W.paged_attention(3, 4, 2, 64, d["keys"].shape[0], 16, d["table"].shape[1], "bf16", 0.125)
+    nodes = [two.nodes[i] for i in (0, 1, 3, 4)] + [dataclasses.replace(two.nodes[5], inputs=(0, 1, 1, 2, 3))]
+    one = W.Program("one", nodes, [4])
+    inputs = {n: d[n] for n in ("q", "keys", "table", "lens")}
+    assert np.array_equal(gpu(one, inputs)["out"], gpu(two, d)["out"])
+
+
+@pytest.mark.gpu
+def test_arrays_of_no_elements():
+    none = np.zeros(0, np.int32)
+    for R, Wd, T, N in ((0, 4, 0, 3), (0, 0, 5, 0), (3, 0, 4, 0), (3, 2, 0, 0)):
+        d = {"lens": np.zeros(R, np.int32), "free": np.zeros(N, np.int32), "off": np.zeros(R + 1, np.int32), "old_lens": np.zeros(R, np.int32),
+             "old": np.zeros((R, Wd), np.int32)}
+        for grow in (False, True):
+            prog = W.block_tables(R, Wd, N, T, 4, grow)
+            want = oracle(prog, d)
+            got = gpu(prog, d)
+            assert all(np.array_equal(got[prog.nodes[o].name], want.values[o]) for o in prog.outputs)
+    d = {"lens": ints(0, 3, 0), "free": none, "off": ints(0, 0, 0, 0)}
+    gpu(W.block_tables(3, 0, 0, 2, 4), d, reported=True)      # a row of no blocks for three tokens
+    for dtype in REAL:
+        for B_, hq, S, Wd in ((0, 4, 8, 2), (2, 0, 8, 2), (2, 4, 0, 2), (2, 4, 8, 0)):
+            prog = W.paged_attention(B_, hq, 2, 16, S, 4, Wd, dtype, 1.0)
+            d = {"q": to_type(np.ones((B_, hq * 16)), dtype), "keys": to_type(np.ones((S, 32)), dtype), "values": to_type(np.ones((S, 32)), dtype),
+                 "table": np.full((B_, Wd), -1, np.int32), "lens": np.zeros(B_, np.int32)}
+            assert not O.widen(gpu(prog, d)["out"], dtype).any()
+            if B_ and hq:
+                d["lens"][1] = 3                             # tokens without a block
+                assert not O.widen(gpu(prog, d, reported=True)["out"], dtype).any()
+
+
 IN_PLACE = {"new_keys": "keys", "new_values": "values", "table": "old", "penalized": "logits"}
 
 

@@ -57,8 +57,8 @@ __device__ __noinline__ int table_entry(const TableArgs& a, int f, int j, int4 r
 // writes a run of a.tile elements of the table, whatever rows they belong to, and adds up for itself what the requests
 // before its first one take: one launch and no waiting on other blocks.  Bound: latency for small tables, then writing the
 // table; the lengths that are read over again (4 R bytes for a block, from L2) are the smaller part as long as
-// R < a.tile.  kTableRows rows at most: where they are shorter than eight elements a block takes fewer elements.
-constexpr int kTableTile = 8192, kTableRows = 1024;
+// R < a.tile.  kTableRows rows at most: where they are shorter than four elements a block takes fewer elements.
+constexpr int kTableTile = 4096, kTableRows = 1024;
 __global__ void __launch_bounds__(kThreads) k_block_table(TableArgs a) {
   __shared__ uint32_t warp_sums[kThreads / 32][2];
   __shared__ int4 rows[kTableRows + 2];                       // kept, end, from (see table_entry)
@@ -122,8 +122,8 @@ int launch_block_table(const ClusterLaunch& L) {
   const bool grow = L.op.n_inputs == 4;
   TableArgs a{report_of(L), slot_ptr<int>(L, 0), slot_ptr<int>(L, 1), grow ? slot_ptr<int>(L, 2) : nullptr, grow ? slot_ptr<int>(L, 3) : nullptr,
               result_ptr<int>(L), t.R, t.C, (int)slot(L, 1).C, 0, divisor((uint32_t)L.op.iparam[0]), divisor((uint32_t)std::max<int64_t>(L.op.shape[1], 1))};
-  // two blocks to an SM, if that leaves each at least four elements a thread
-  const long long even = (count + 2 * sm_count() - 1) / (2 * sm_count());
+  // six blocks to an SM, if that leaves each at least four elements a thread
+  const long long even = (count + 6 * sm_count() - 1) / (6 * sm_count());
   a.tile = (int)std::min<long long>(kTableTile, (even + 4 * kThreads - 1) / (4 * kThreads) * (4 * kThreads));
   a.tile = (int)std::min<int64_t>(a.tile, kTableRows * (int64_t)a.W);
   return launch_following(k_block_table, dim3((unsigned)std::max<long long>((count + a.tile - 1) / std::max(a.tile, 1), 1)), kThreads, 0, L.stream, a);
@@ -169,8 +169,36 @@ __device__ __forceinline__ int slot_of(const SlotArgs& a, const int* off, const 
   return (int)at;
 }
 
-// A block maps a run of tokens, a thread one, four or sixteen side by side (which for prompts mostly are one request's, in
-// one block or two where blocks are no shorter).  The offsets and lengths of their requests are brought into shared memory, those of all
+// Slots of tokens t .. t+3, of which the first is held by request lo or a later one.
+__device__ __forceinline__ int4 four_slots(const SlotArgs& a, const int* off, const int* lens, int first, int rows, int lo, int t, int t1, bool& bad) {
+  if (lo < rows && t + 4 <= t1 && off[lo] <= t && t + 4 <= off[lo + 1] && a.block.d >= 4 && lens[lo] >= 0) {
+    // all of one request, in one block or in two
+    const uint32_t left = (uint32_t)off[lo + 1] - (uint32_t)t, p = (uint32_t)lens[lo] - left;
+    const uint32_t q = p / a.block, inside = p - q * a.block.d, here = a.block.d - inside;         // tokens of the first block
+    const bool two = here < 4;
+    if ((uint32_t)lens[lo] >= left && q + two < (uint32_t)a.W) {
+      const int* row = a.table + (size_t)(first + lo) * a.W + q;
+      const int page = row[0], behind = two ? row[1] : page;
+      const long long at = (long long)page * a.block.d + inside, next = two ? (long long)behind * a.block.d - here : at;
+      if (page >= 0 && behind >= 0 && at + 4 <= 0x7FFFFFFFll && next + 4 <= 0x7FFFFFFFll)
+        return make_int4((int)at, (1 < here ? (int)at : (int)next) + 1, (2 < here ? (int)at : (int)next) + 2, (3 < here ? (int)at : (int)next) + 3);
+    }
+  }
+  int v[4] = {-1, -1, -1, -1};
+#pragma unroll 1
+  for (int k = 0; k < 4 && t + k < t1; ++k) {
+    while (lo < rows && off[lo + 1] <= t + k) ++lo;
+    const int x = slot_of(a, off, lens, first, rows, lo, t + k, bad);
+    if (k == 0) v[0] = x;
+    else if (k == 1) v[1] = x;
+    else if (k == 2) v[2] = x;
+    else v[3] = x;
+  }
+  return make_int4(v[0], v[1], v[2], v[3]);
+}
+
+// A block maps a run of tokens, a thread one, or a warp 512 in rows of four to a lane (for prompts mostly one request's:
+// then it is looked for once).  The offsets and lengths of their requests are brought into shared memory, those of all
 // requests where that is few, else those from the first to the last token's, which the first warps look for; every thread
 // finds the request of its tokens there.  (Between two tokens may lie more empty requests than there is room for: then the
 // offsets are searched where they are.)  Bound: latency, a chain of three to five dependent reads; for prompts writing
@@ -216,58 +244,50 @@ __global__ void __launch_bounds__(kThreads) k_slot_map(SlotArgs a) {
     low = min(range[0], rows), high = max(min(range[1], rows), low);
   }
   bool bad = false;
-  const int t = t0 + PER * threadIdx.x;
-  if (t >= t1) return;
-  int lo = low, hi = high;                                             // (the request of the last token is found by elimination)
-  while (lo < hi) {
-    const int mid = (lo + hi) >> 1;
-    if (off[mid + 1] <= t) lo = mid + 1;
-    else hi = mid;
-  }
-  if constexpr (PER == 1) {
-    a.out[t] = slot_of(a, off, lens, first, rows, lo, t, bad);
-  } else {
-    // all of one request, in one block or in two
-    bool one = lo < rows && t + PER <= t1 && off[lo] <= t && t + PER <= off[lo + 1] && a.block.d >= PER && lens[lo] >= 0;
-    if (one) {
-      const uint32_t left = (uint32_t)off[lo + 1] - (uint32_t)t, p = (uint32_t)lens[lo] - left;
-      const uint32_t q = p / a.block, inside = p - q * a.block.d, here = a.block.d - inside;       // tokens of the first block
-      const bool two = here < PER;
-      one = (uint32_t)lens[lo] >= left && q + two < (uint32_t)a.W;
-      const int* row = a.table + (size_t)(first + lo) * a.W + q;
-      const int page = one ? row[0] : -1, behind = one && two ? row[1] : page;
-      const long long at = (long long)page * a.block.d + inside, next = two ? (long long)behind * a.block.d - here : at;
-      one = one && page >= 0 && behind >= 0 && at + PER <= 0x7FFFFFFFll && next + PER <= 0x7FFFFFFFll;
-      if (one) {
-        const int v0 = (int)at, v1 = (int)next;
-        int4* to = reinterpret_cast<int4*>(a.out + t);
-#pragma unroll
-        for (int k = 0; k < PER; k += 4)
-          to[k / 4] = make_int4((k < here ? v0 : v1) + k, (k + 1 < here ? v0 : v1) + k + 1, (k + 2 < here ? v0 : v1) + k + 2, (k + 3 < here ? v0 : v1) + k + 3);
-      }
+  const auto holder = [&](int t, int from) {                           // (the request of the last token is found by elimination)
+    int lo = from, hi = high;
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1;
+      if (off[mid + 1] <= t) lo = mid + 1;
+      else hi = mid;
     }
-    if (!one) {
+    return lo;
+  };
+  if constexpr (PER == 1) {
+    const int t = t0 + threadIdx.x;
+    if (t < t1) a.out[t] = slot_of(a, off, lens, first, rows, holder(t, low), t, bad);
+  } else {
+    const int from = t0 + (threadIdx.x & ~31) * PER;                   // the warp's first token
+    if (from >= t1) return;
+    const int request = holder(from, low);
+    const bool one = request < rows && off[request] <= from && min((long long)from + 32 * PER, (long long)t1) <= off[request + 1];
 #pragma unroll 1
-      for (int k = 0; k < PER && t + k < t1; ++k) {
-        while (lo < rows && off[lo + 1] <= t + k) ++lo;
-        a.out[t + k] = slot_of(a, off, lens, first, rows, lo, t + k, bad);
+    for (int g = 0; g < PER / 4; ++g) {
+      const int t = from + (g * 32 + (threadIdx.x & 31)) * 4;
+      if (t >= t1) break;
+      const int4 v = four_slots(a, off, lens, first, rows, one ? request : holder(t, request), t, t1, bad);
+      if (t + 4 <= t1) *reinterpret_cast<int4*>(a.out + t) = v;
+      else {
+        a.out[t] = v.x;
+        if (t + 1 < t1) a.out[t + 1] = v.y;
+        if (t + 2 < t1) a.out[t + 2] = v.z;
       }
     }
   }
   if (bad) raise_index(a.report);
 }
 
-// Tokens up to which every thread takes one: a step's tokens are of a request each, so that sixteen side by side would
-// read the table one after the other.
+// Tokens up to which every thread takes one: a step's tokens are of a request each, so that four side by side would read
+// the table one after the other.
 constexpr int kSingleTokens = 1 << 16;
 int launch_slot_map(const ClusterLaunch& L) {
   const dev::NodeArg& table = slot(L, 0);
   SlotArgs a{report_of(L), slot_ptr<int>(L, 0), slot_ptr<int>(L, 1), slot_ptr<int>(L, 2), result_ptr<int>(L),
              table.R, table.C, (int)L.op.shape[0], divisor((uint32_t)L.op.iparam[0])};
   if (a.T == 0) return ACC_OK;
-  const int per = a.T <= kSingleTokens ? 1 : a.block.d >= 16 ? 16 : 4;
-  const int tile = per * kThreads;
-  return launch_following(per == 1 ? k_slot_map<1> : per == 4 ? k_slot_map<4> : k_slot_map<16>, dim3((unsigned)(((long long)a.T + tile - 1) / tile)), kThreads, 0, L.stream, a);
+  const bool single = a.T <= kSingleTokens;
+  const int tile = single ? kThreads : 16 * kThreads;
+  return launch_following(single ? k_slot_map<1> : k_slot_map<16>, dim3((unsigned)(((long long)a.T + tile - 1) / tile)), kThreads, 0, L.stream, a);
 }
 
 const Register block_table(ACC_BLOCK_TABLE, "k_block_table", no_scratch, launch_block_table);

@@ -219,10 +219,11 @@ __device__ __forceinline__ void finish_unit(const AttentionArgs& a, int b, int k
   }
 }
 
-// Adds up the records of a split unit.  Few records: a warp to a head, a lane to four dimensions.  Many: the block's warps
-// share the records of 32 dimensions of a head, which a lane in eight reads four of; a block to each of these pieces where
-// units are few (a.join_rows = 1), else one block to eight heads.
-constexpr int kJoinThreads = 256, kJoinWarps = kJoinThreads / 32, kManyRecords = 16, kMaxGrid = 1024, kPiece = 32;
+// Adds up the records of a split unit.  Few units (a.join_rows = 1), so many records each: a block to 32 dimensions of a
+// head, whose records its warps share, a lane in eight four dimensions of one.  Else a block to eight heads, a warp to each,
+// a lane to four dimensions, eight records on their way at a time: lengths differ, and so one unit may have many records
+// where most have few (4 requests of up to 6000 tokens, all of a block's warps on one head after the other: 26 us, so 4).
+constexpr int kJoinThreads = 256, kJoinWarps = kJoinThreads / 32, kMaxGrid = 1024, kPiece = 32;
 template <class T, int DP, int ROWS, int WAYS>
 __global__ void __launch_bounds__(kJoinThreads) k_join(AttentionArgs a) {
   constexpr int HEADS = ROWS * WAYS, VECS = (DP / 4 + 31) / 32;
@@ -247,88 +248,99 @@ __global__ void __launch_bounds__(kJoinThreads) k_join(AttentionArgs a) {
 #pragma unroll
     for (int k = 0; k < 4; ++k) out[k] = narrow<T>(top == -INFINITY ? 0.0f : __fdiv_rn(z[k], l));
   };
-  if (n <= kManyRecords && a.join_rows > 1) {
+  constexpr int BATCH = 8;
+  if (a.join_rows > 1) {
     for (int h = r0 + warp; h < r0 + a.join_rows; h += kJoinWarps) {
       if (h % ROWS >= a.group - head0) continue;
-      const float t = lane < n ? from.tops[at(lane, h)] : -INFINITY, share = lane < n ? from.weights[at(lane, h)] : 0.0f;
-      float top = t;
+      float top = -INFINITY;
+      for (int i = lane; i < n; i += 32) top = fmaxf(top, from.tops[at(i, h)]);
 #pragma unroll
       for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
-      const float w = power2(t - (top == -INFINITY ? 0.0f : top));
+      const float ref = top == -INFINITY ? 0.0f : top;
       float4 y[VECS] = {};
       float l = 0;
-#pragma unroll 4
-      for (int i = 0; i < n; ++i) {
-        const float wi = __shfl_sync(~0u, w, i);
-        l = fmaf(wi, __shfl_sync(~0u, share, i), l);
+#pragma unroll 1
+      for (int i0 = 0; i0 < n; i0 += BATCH) {
+        float4 x[BATCH][VECS];
+        float w[BATCH], share[BATCH];
 #pragma unroll
-        for (int v = 0; v < VECS; ++v)
-          if ((lane + 32 * v) * 4 < DP) add(y[v], wi, *reinterpret_cast<const float4*>(from.sums + at(i, h) * DP + (lane + 32 * v) * 4));
+        for (int k = 0; k < BATCH; ++k) {
+          const bool is = i0 + k < n;
+          const size_t row = at(is ? i0 + k : 0, h);
+          w[k] = is ? from.tops[row] : -INFINITY;
+          share[k] = is ? from.weights[row] : 0.0f;
+#pragma unroll
+          for (int v = 0; v < VECS; ++v)
+            x[k][v] = is && (lane + 32 * v) * 4 < DP ? *reinterpret_cast<const float4*>(from.sums + row * DP + (lane + 32 * v) * 4) : make_float4(0, 0, 0, 0);
+        }
+#pragma unroll
+        for (int k = 0; k < BATCH; ++k) {
+          const float wk = power2(w[k] - ref);
+          l = fmaf(wk, share[k], l);
+#pragma unroll
+          for (int v = 0; v < VECS; ++v) add(y[v], wk, x[k][v]);
+        }
       }
 #pragma unroll
       for (int v = 0; v < VECS; ++v) write(h, (lane + 32 * v) * 4, y[v], l, top);
     }
     return;
   }
-  constexpr int BATCH = 8, STEP = 4 * kJoinWarps;          // four records to a warp at a time
+  constexpr int STEP = 4 * kJoinWarps;                     // four records to a warp at a time
   const int mine = warp * 4 + (lane >> 3);
-  for (int h = r0; h < r0 + a.join_rows; ++h) {
-    if (h % ROWS >= a.group - head0) continue;
-    for (int piece = blockIdx.z; piece < DP / kPiece; piece += gridDim.z) {
-      const int d = piece * kPiece + (lane & 7) * 4;
-      const auto load = [&](int i) { return i < n ? *reinterpret_cast<const float4*>(from.sums + at(i, h) * DP + d) : make_float4(0, 0, 0, 0); };
-      float4 ahead[BATCH];                                 // on their way while the maxima are compared
+  const int h = r0;
+  if (h % ROWS >= a.group - head0) return;
+  const int d = blockIdx.z * kPiece + (lane & 7) * 4;
+  const auto load = [&](int i) { return i < n ? *reinterpret_cast<const float4*>(from.sums + at(i, h) * DP + d) : make_float4(0, 0, 0, 0); };
+  float4 ahead[BATCH];                                 // on their way while the maxima are compared
 #pragma unroll
-      for (int k = 0; k < BATCH; ++k) ahead[k] = load(mine + k * STEP);
-      float top = -INFINITY;
-      for (int i = threadIdx.x; i < n; i += kJoinThreads) {
-        weight[i] = from.tops[at(i, h)];
-        top = fmaxf(top, weight[i]);
-      }
+  for (int k = 0; k < BATCH; ++k) ahead[k] = load(mine + k * STEP);
+  float top = -INFINITY;
+  for (int i = threadIdx.x; i < n; i += kJoinThreads) {
+    weight[i] = from.tops[at(i, h)];
+    top = fmaxf(top, weight[i]);
+  }
 #pragma unroll
-      for (int k = 16; k > 0; k >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, k));
-      if (lane == 0) tops[warp] = top;
-      __syncthreads();
+  for (int k = 16; k > 0; k >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, k));
+  if (lane == 0) tops[warp] = top;
+  __syncthreads();
 #pragma unroll
-      for (int w = 0; w < kJoinWarps; ++w) top = fmaxf(top, tops[w]);
-      const float ref = top == -INFINITY ? 0.0f : top;
-      float l = 0;
-      for (int i = threadIdx.x; i < n; i += kJoinThreads) {
-        weight[i] = power2(weight[i] - ref);
-        l = fmaf(weight[i], from.weights[at(i, h)], l);
-      }
+  for (int w = 0; w < kJoinWarps; ++w) top = fmaxf(top, tops[w]);
+  const float ref = top == -INFINITY ? 0.0f : top;
+  float l = 0;
+  for (int i = threadIdx.x; i < n; i += kJoinThreads) {
+    weight[i] = power2(weight[i] - ref);
+    l = fmaf(weight[i], from.weights[at(i, h)], l);
+  }
 #pragma unroll
-      for (int k = 16; k > 0; k >>= 1) l += __shfl_xor_sync(~0u, l, k);
-      if (lane == 0) shares[warp] = l;
-      __syncthreads();
-      float4 y = make_float4(0, 0, 0, 0);
-      for (int i0 = mine; i0 < n; i0 += BATCH * STEP) {
-        if (i0 != mine)
+  for (int k = 16; k > 0; k >>= 1) l += __shfl_xor_sync(~0u, l, k);
+  if (lane == 0) shares[warp] = l;
+  __syncthreads();
+  float4 y = make_float4(0, 0, 0, 0);
+  for (int i0 = mine; i0 < n; i0 += BATCH * STEP) {
+    if (i0 != mine)
 #pragma unroll
-          for (int k = 0; k < BATCH; ++k) ahead[k] = load(i0 + k * STEP);
+      for (int k = 0; k < BATCH; ++k) ahead[k] = load(i0 + k * STEP);
 #pragma unroll
-        for (int k = 0; k < BATCH; ++k)
-          if (i0 + k * STEP < n) add(y, weight[i0 + k * STEP], ahead[k]);
-      }
+    for (int k = 0; k < BATCH; ++k)
+      if (i0 + k * STEP < n) add(y, weight[i0 + k * STEP], ahead[k]);
+  }
 #pragma unroll
-      for (int k = 8; k < 32; k <<= 1) {
-        y.x += __shfl_xor_sync(~0u, y.x, k), y.y += __shfl_xor_sync(~0u, y.y, k);
-        y.z += __shfl_xor_sync(~0u, y.z, k), y.w += __shfl_xor_sync(~0u, y.w, k);
-      }
-      if (lane < kPiece / 4) sums[warp][lane] = y;
-      __syncthreads();
-      if (threadIdx.x < kPiece / 4) {
-        l = 0;
-        y = make_float4(0, 0, 0, 0);
+  for (int k = 8; k < 32; k <<= 1) {
+    y.x += __shfl_xor_sync(~0u, y.x, k), y.y += __shfl_xor_sync(~0u, y.y, k);
+    y.z += __shfl_xor_sync(~0u, y.z, k), y.w += __shfl_xor_sync(~0u, y.w, k);
+  }
+  if (lane < kPiece / 4) sums[warp][lane] = y;
+  __syncthreads();
+  if (threadIdx.x < kPiece / 4) {
+    l = 0;
+    y = make_float4(0, 0, 0, 0);
 #pragma unroll
-        for (int w = 0; w < kJoinWarps; ++w) {
-          l += shares[w];
-          add(y, 1.0f, sums[w][lane]);
-        }
-        write(h, d, y, l, top);
-      }
-      __syncthreads();
+    for (int w = 0; w < kJoinWarps; ++w) {
+      l += shares[w];
+      add(y, 1.0f, sums[w][lane]);
     }
+    write(h, d, y, l, top);
   }
 }
 
@@ -963,7 +975,7 @@ int run(const ClusterLaunch& L, K kernel, std::atomic<uint64_t>& allowed) {
   const int rc = allow_shared(kernel, S::kShared, allowed);
   if (rc != ACC_OK) return rc;
   const int heads = S::kRows * S::kWays, pieces = DP / kPiece;
-  a.join_rows = joins_of(a) * heads * pieces <= 2 * sm_count() ? 1 : std::min(8, heads);
+  a.join_rows = joins_of(a) * heads * pieces <= 8 * sm_count() ? 1 : std::min(8, heads);
   // (not launched early: beside the kernel before it an SM is divided for less shared memory, and keeps to that while the
   // blocks that did fit run; 31 windows of 4096 tokens, back to back: 101 us, launched early 154)
   kernel<<<grid, kThreads, S::kShared, L.stream>>>(a);

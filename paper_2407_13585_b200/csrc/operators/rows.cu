@@ -23,9 +23,10 @@ template <> struct Unit<16> { using type = uint4; };
 template <> struct Unit<4> { using type = uint32_t; };
 template <> struct Unit<2> { using type = uint16_t; };
 
-constexpr int kUnitsPerLane = 4;
+constexpr int kUnitsPerLane = 8;
 
-// A warp moves 32 x 4 units of a row (2 KB of 16-byte units).  Rows for one slot: the last one stays, whatever the order
+// A warp moves 32 x 8 units of a row (4 KB of 16-byte units; 12000 rows of 4 KB, twice: 38 us, with 4 units to a lane 42).
+// Bound: memory, rows read in order and written at random places.  Rows for one slot: the last one stays, whatever the order
 // the warps run in, because every warp looks for a later row of its slot before it stores (its row is on the way
 // meanwhile), or finds the slot's last row in `owner`.
 template <int BYTES>

@@ -413,8 +413,13 @@ __device__ __forceinline__ uint32_t ask_for(const AttentionArgs& a, const Cursor
 
 template <class T> struct Half;
 template <> struct Half<__half> {
-  // weights are held as 2^(s - m + 12), so that the smallest that count are no subnormal numbers of the type
-  static constexpr float kRaise = 12.0f;
+  // The type ends at 2^16 and its steps at 2^-24.  Weights are raised by 2^15: two parts hold one of 2^-18 of the maximum or
+  // more to 2^-22.  Those below (kSmall) are raised by another 2^18 and have products of their own, in tiles that have any:
+  // down to 2^-36 they are held to 2^-22 as well, and what is lost of smaller ones is 2^-58 of the maximum at most.  (Raised
+  // by 2^12 and without products of their own, weights of 2^-30 were off by 2^-8 and those of 2^-38 were nothing.  Where every
+  // tile has small ones, 31 windows of 20 heads of 80 take 110 us in place of 97, 2 GB under sixteen heads of 256 718, so 470.)
+  static constexpr int kParts = 2;
+  static constexpr float kRaise = 32768.0f, kSmall = 0x1p-3f, kRaiseSmall = 0x1p18f, kNothing = 0x1p-43f;
   static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
     const __half2 v = __floats2half2_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&v);
@@ -426,7 +431,8 @@ template <> struct Half<__half> {
   }
 };
 template <> struct Half<__nv_bfloat16> {
-  static constexpr float kRaise = 0.0f;
+  static constexpr int kParts = 2;
+  static constexpr float kRaise = 1.0f, kSmall = 0.0f;
   static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
     const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&v);
@@ -467,8 +473,8 @@ struct HalfShape {
 // values^T x weights (16 dimensions x 8 heads): the heads are the eight columns of a matrix instruction both times, and a
 // lane's scores, maxima and sums belong to the same two heads, so that nothing is exchanged to rescale them.  The weights
 // go from one shape to the other by transposing 8 x 8 matrices, as two 16-bit parts each (value and remainder), which
-// holds them to 2^-17 (bf16) or 2^-22 (fp16): one part alone would cost up to 2^-9 of sum w |v|, more than the rounding
-// of the result where values cancel, and the second product is hidden behind the loads.
+// holds them to 2^-17 (bf16) or 2^-22 (fp16, see Half): one part alone would cost up to 2^-9 of sum w |v|, more than the
+// rounding of the result where values cancel, and the second product is hidden behind the loads.
 template <class T, int DP, int NT, int WAYS>
 __global__ void __launch_bounds__(kThreads, HalfShape<DP, NT, WAYS>::kResident) k_attention_half(AttentionArgs a) {
   using H = Half<T>;
@@ -569,7 +575,7 @@ __global__ void __launch_bounds__(kThreads, HalfShape<DP, NT, WAYS>::kResident) 
           for (int n = 0; n < NT; ++n) H::mma(k & 1 ? odd[t][n] : s[t][n], f, q[n][k][0], q[n][k][1]);
         }
       }
-      uint32_t w_hi[MT][NT][2], w_lo[MT][NT][2];
+      uint32_t parts[H::kParts][MT][NT][2];
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
         float top[2] = {-INFINITY, -INFINITY};
@@ -595,22 +601,65 @@ __global__ void __launch_bounds__(kThreads, HalfShape<DP, NT, WAYS>::kResident) 
           l[n][0] *= f0, l[n][1] *= f1;
           m[n][0] = top[0], m[n][1] = top[1];
         }
+        // a weight as the sum of 16-bit parts, each transposed to what the second product takes
+        const auto split = [](const float* w, auto&& part) {
+          float rest[4] = {w[0], w[1], w[2], w[3]};
+#pragma unroll
+          for (int p = 0; p < H::kParts; ++p)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              const uint32_t x = H::pack(rest[2 * i], rest[2 * i + 1]);
+              const float2 back = H::unpack(x);
+              rest[2 * i] -= back.x, rest[2 * i + 1] -= back.y;
+              part(p, i) = transpose_matrix(x);
+            }
+        };
+        float w[MT][4];
 #pragma unroll
         for (int t = 0; t < MT; ++t) {
-          float w[4];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) w[i] = power2(s[t][n][i] - m[n][i & 1] + H::kRaise);
-          l[n][0] += w[0] + w[2];
-          l[n][1] += w[1] + w[3];
+          for (int i = 0; i < 4; ++i) w[t][i] = power2(s[t][n][i] - m[n][i & 1]) * H::kRaise;
+          l[n][0] += w[t][0] + w[t][2];
+          l[n][1] += w[t][1] + w[t][3];
+        }
+        if constexpr (H::kSmall > 0) {
+          // (of numbers that are not negative, in the order of their patterns)
+          const uint32_t least = __float_as_uint(H::kNothing);
+          uint32_t above = ~0u;
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const uint32_t hi = H::pack(w[2 * i], w[2 * i + 1]);
-            const float2 back = H::unpack(hi);
-            const uint32_t lo = H::pack(w[2 * i] - back.x, w[2 * i + 1] - back.y);
-            w_hi[t][n][i] = transpose_matrix(hi);
-            w_lo[t][n][i] = transpose_matrix(lo);
+          for (int t = 0; t < MT; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) above = min(above, __float_as_uint(w[t][i]) - least);
+          if (__any_sync(~0u, above < __float_as_uint(H::kSmall) - least)) {
+            uint32_t small[H::kParts][MT][2];
+#pragma unroll
+            for (int t = 0; t < MT; ++t) {
+              float x[4];
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const bool is = w[t][i] < H::kSmall;
+                x[i] = is ? w[t][i] * H::kRaiseSmall : 0.0f;
+                w[t][i] = is ? 0.0f : w[t][i];
+              }
+              split(x, [&](int p, int i) -> uint32_t& { return small[p][t][i]; });
+            }
+#pragma unroll
+            for (int k = 0; k < DP / 16; ++k) {
+              float c[4] = {0, 0, 0, 0};
+#pragma unroll
+              for (int t = 0; t < MT; ++t) {
+                uint32_t f[4];
+                load_matrices_transposed(f, values + (t * 16 + v_row) * S::kRowBytes + (((k * 2 + v_half) ^ (v_row & 7)) << 4));
+#pragma unroll
+                for (int p = 0; p < H::kParts; ++p) H::mma(c, f, small[p][t][0], small[p][t][1]);
+              }
+#pragma unroll
+              for (int i = 0; i < 4; ++i) o[n][k][i] = fmaf(c[i], 1 / H::kRaiseSmall, o[n][k][i]);
+            }
           }
         }
+#pragma unroll
+        for (int t = 0; t < MT; ++t) split(w[t], [&](int p, int i) -> uint32_t& { return parts[p][t][n][i]; });
       }
 #pragma unroll
       for (int k = 0; k < DP / 16; ++k) {
@@ -619,10 +668,9 @@ __global__ void __launch_bounds__(kThreads, HalfShape<DP, NT, WAYS>::kResident) 
           uint32_t f[4];
           load_matrices_transposed(f, values + (t * 16 + v_row) * S::kRowBytes + (((k * 2 + v_half) ^ (v_row & 7)) << 4));
 #pragma unroll
-          for (int n = 0; n < NT; ++n) {
-            H::mma(o[n][k], f, w_hi[t][n][0], w_hi[t][n][1]);
-            H::mma(o[n][k], f, w_lo[t][n][0], w_lo[t][n][1]);
-          }
+          for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int p = 0; p < H::kParts; ++p) H::mma(o[n][k], f, parts[p][t][n][0], parts[p][t][n][1]);
         }
       }
     }

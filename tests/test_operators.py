@@ -1033,3 +1033,48 @@ def test_operators_end_to_end_from_host_buffers():
     assert up == sum(t.numel() * t.element_size() for t in host.values()) and down == back.numel() * 2
     _check_step(prog, d, b.outputs(), "f16")
     assert torch.equal(back, b.t["out"].cpu())
+
+
+# ---- weights and numbers at the ends of their ranges -----------------------------------------------------------------
+
+def _powers_of_two(prog_args, d, dtype):
+    """A program whose weights are 2^(q.k) exactly as long as q.k is held exactly: scale = ln 2."""
+    B_, hq, hk, D, block = prog_args
+    return W.paged_attention(B_, hq, hk, D, d["keys"].shape[0], block, d["table"].shape[1], dtype, float(np.log(2.0)))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", REAL)
+@pytest.mark.parametrize("hq,hk,D,B_", [(2, 1, 64, 14), (16, 1, 128, 14), (12, 4, 80, 42), (9, 1, 256, 14), (64, 4, 64, 42)])
+def test_paged_attention_to_tokens_of_small_weight(hq, hk, D, B_, dtype):
+    """One token takes nearly all the weight and has values of zero, so that the result comes from the others, whose weights
+    are 2^-17.25 to 2^-50.25 of its: held to as many bits as the large ones.  A third of the tokens lie in between, with
+    values of zero too.
+
+    Scores are exact.  Relative to sum w |v|, with u = 2^-23: the exponential 2^-22, in numerator and denominator; n + 32
+    additions for the denominator, and for the numerator (sixteen products and a sum per matrix instruction, three parts, each
+    addend cut off at u / 2 of the largest) 3 * 17 / 16 / 2 < 2 times as many; weights in fp16 parts 2^-22 down to 2^-36 and 2^-58
+    of the largest below; the result half a step."""
+    exponents = [17.25, 18.25, 19.25, 22.25, 23.25, 26.25, 28.25, 30.25, 33.25, 35.25, 36.25, 38.25, 42.25, 50.25]
+    rng = np.random.default_rng(D)
+    n, block = 300, 16
+    d = _attention_inputs(rng, B_, hq, hk, D, block, [n] * B_, dtype)
+    q, keys, values = np.zeros((B_, hq, D)), np.zeros((d["keys"].shape[0], hk, D)), rng.uniform(1000, 60000, (d["keys"].shape[0], hk, D))
+    q[:, :, 0] = 1
+    p = np.arange(n)
+    for b in range(B_):
+        at = d["table"][b, p // block] * block + p % block
+        keys[at, :, 0] = -exponents[b % len(exponents)]
+        keys[at[::3], :, 0] = -12.5
+        keys[at[(37 * b) % n], :, 0] = 0
+        values[at[::3]] = values[at[(37 * b) % n]] = 0
+    d |= {"q": to_type(q.reshape(B_, -1), dtype), "keys": to_type(keys.reshape(-1, hk * D), dtype), "values": to_type(values.reshape(-1, hk * D), dtype)}
+    prog = _powers_of_two((B_, hq, hk, D, block), d, dtype)
+    want = oracle(prog, d)
+    exact, scale_of = want.exact[5], want.abs_sum[5]
+    assert np.all(exact > 0)
+    e = np.array([exponents[b % len(exponents)] for b in range(B_)])[:, None]
+    split = np.maximum(2.0 ** -22, 2.0 ** (e - 58)) if dtype == "f16" else 0.0
+    bound = scale_of * (2 * 2.0 ** -22 + 3 * (n + 32) * 2.0 ** -23 + split) + exact * EPS[dtype] / 2 + TINY[dtype]
+    err = np.abs(O.widen(gpu(prog, d)["out"], dtype) - exact) / (bound * (1 + 2.0 ** -7))
+    assert np.all(err <= 1), [(float(x), float(y)) for x, y in zip(e[:len(exponents), 0], err.max(1))]

@@ -431,7 +431,8 @@ template <> struct Half<__half> {
   }
 };
 template <> struct Half<__nv_bfloat16> {
-  static constexpr int kParts = 2;
+  // eight bits each: all of a 32-bit weight, if it is above 2^-110 of the maximum
+  static constexpr int kParts = 3;
   static constexpr float kRaise = 1.0f, kSmall = 0.0f;
   static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
     const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
@@ -472,9 +473,10 @@ struct HalfShape {
 // Scores as keys x queries (16 tokens x 8 heads, products of 16-bit values exact, sums in 32 bits), weighted values as
 // values^T x weights (16 dimensions x 8 heads): the heads are the eight columns of a matrix instruction both times, and a
 // lane's scores, maxima and sums belong to the same two heads, so that nothing is exchanged to rescale them.  The weights
-// go from one shape to the other by transposing 8 x 8 matrices, as two 16-bit parts each (value and remainder), which
-// holds them to 2^-17 (bf16) or 2^-22 (fp16, see Half): one part alone would cost up to 2^-9 of sum w |v|, more than the
-// rounding of the result where values cancel, and the second product is hidden behind the loads.
+// go from one shape to the other by transposing 8 x 8 matrices, as 16-bit parts that add up to them: three in bf16, all their
+// bits, two in fp16, to 2^-22 (see Half).  Fewer would cost 2^-17 (bf16) of sum w |v|, more than the rounding of the result where
+// values cancel.  Further products are hidden behind the loads with up to eight query heads a key head; with sixteen the third
+// one takes its time (2 GB of bf16 heads of 256 473 us with two, 507 with three; of 128 353 and 375, of 64 355 and 376).
 template <class T, int DP, int NT, int WAYS>
 __global__ void __launch_bounds__(kThreads, HalfShape<DP, NT, WAYS>::kResident) k_attention_half(AttentionArgs a) {
   using H = Half<T>;
@@ -662,15 +664,19 @@ __global__ void __launch_bounds__(kThreads, HalfShape<DP, NT, WAYS>::kResident) 
         for (int t = 0; t < MT; ++t) split(w[t], [&](int p, int i) -> uint32_t& { return parts[p][t][n][i]; });
       }
 #pragma unroll
-      for (int k = 0; k < DP / 16; ++k) {
+      for (int k = 0; k < DP / 16; k += 2) {   // two at a time: sums that do not wait for one another (551 us for 507 above)
 #pragma unroll
         for (int t = 0; t < MT; ++t) {
-          uint32_t f[4];
-          load_matrices_transposed(f, values + (t * 16 + v_row) * S::kRowBytes + (((k * 2 + v_half) ^ (v_row & 7)) << 4));
+          uint32_t f[2][4];
 #pragma unroll
-          for (int n = 0; n < NT; ++n)
+          for (int i = 0; i < 2; ++i)
+            load_matrices_transposed(f[i], values + (t * 16 + v_row) * S::kRowBytes + ((((k + i) * 2 + v_half) ^ (v_row & 7)) << 4));
 #pragma unroll
-            for (int p = 0; p < H::kParts; ++p) H::mma(o[n][k], f, parts[p][t][n][0], parts[p][t][n][1]);
+          for (int p = 0; p < H::kParts; ++p)
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+              for (int n = 0; n < NT; ++n) H::mma(o[n][k + i], f[i], parts[p][t][n][0], parts[p][t][n][1]);
         }
       }
     }

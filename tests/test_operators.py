@@ -1078,3 +1078,37 @@ def test_paged_attention_to_tokens_of_small_weight(hq, hk, D, B_, dtype):
     bound = scale_of * (2 * 2.0 ** -22 + 3 * (n + 32) * 2.0 ** -23 + split) + exact * EPS[dtype] / 2 + TINY[dtype]
     err = np.abs(O.widen(gpu(prog, d)["out"], dtype) - exact) / (bound * (1 + 2.0 ** -7))
     assert np.all(err <= 1), [(float(x), float(y)) for x, y in zip(e[:len(exponents), 0], err.max(1))]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", REAL)
+@pytest.mark.parametrize("B_", [4, 40])
+def test_paged_attention_to_values_that_cancel(B_, dtype):
+    """Two tokens whose weighted values are opposite to within 2^-8 of one of them: what is left shows the bits of a weight that
+    rounding a larger result would hide.
+
+    Scores are exact, the first weight is 1.  Relative to sum w |v|, with u = 2^-23: the second weight 2^-22, eight additions
+    that are not of zeros (two in the first matrix instruction, three in those of further parts), fp16 parts 2^-22; the
+    quotient and the denominator 4 u and the rounding half a step, of the result."""
+    hq = hk = 8
+    D, block = 64, 16
+    rng = np.random.default_rng(B_)
+    d = _attention_inputs(rng, B_, hq, hk, D, block, [2] * B_, dtype)
+    scores = O.widen(to_type(-2 * rng.random((B_, hq)), dtype), dtype)
+    q, keys, values = np.zeros((B_, hq, D)), np.zeros((d["keys"].shape[0], hk, D)), np.zeros((d["keys"].shape[0], hk, D))
+    q[:, :, 0] = scores
+    small = np.arange(1, 256)
+    for b in range(B_):
+        at = d["table"][b, 0] * block
+        keys[at + 1, :, 0] = 1
+        for h in range(hk):
+            products = 2.0 ** scores[b, h] * small
+            best = np.argsort(np.abs(products - np.round(products)) / small)[:D]
+            values[at + 1, h], values[at, h] = small[best], -np.round(products)[best]
+    d |= {"q": to_type(q.reshape(B_, -1), dtype), "keys": to_type(keys.reshape(-1, hk * D), dtype), "values": to_type(values.reshape(-1, hk * D), dtype)}
+    prog = _powers_of_two((B_, hq, hk, D, block), d, dtype)
+    want = oracle(prog, d)
+    exact, scale_of = want.exact[5], want.abs_sum[5]
+    bound = scale_of * (2.0 ** -22 + 8 * 2.0 ** -23 + (2.0 ** -22 if dtype == "f16" else 0.0)) + np.abs(exact) * (EPS[dtype] / 2 + 4 * 2.0 ** -23) + TINY[dtype]
+    err = np.abs(O.widen(gpu(prog, d)["out"], dtype) - exact) / (bound * (1 + 2.0 ** -7))
+    assert np.all(err <= 1), float(err.max())

@@ -417,7 +417,7 @@ template <> struct Half<__half> {
   // more to 2^-22.  Those below (kSmall) are raised by another 2^18 and have products of their own, in tiles that have any:
   // down to 2^-36 they are held to 2^-22 as well, and what is lost of smaller ones is 2^-58 of the maximum at most.  (Raised
   // by 2^12 and without products of their own, weights of 2^-30 were off by 2^-8 and those of 2^-38 were nothing.  Where every
-  // tile has small ones, 31 windows of 20 heads of 80 take 110 us in place of 97, 2 GB under sixteen heads of 256 718, so 470.)
+  // tile has small ones, 31 windows of 20 heads of 80 take 110 us in place of 98, 2 GB under sixteen heads of 256 875, so 620.)
   static constexpr int kParts = 2;
   static constexpr float kRaise = 32768.0f, kSmall = 0x1p-3f, kRaiseSmall = 0x1p18f, kNothing = 0x1p-43f;
   static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
@@ -425,6 +425,11 @@ template <> struct Half<__half> {
     return *reinterpret_cast<const uint32_t*>(&v);
   }
   static __device__ __forceinline__ float2 unpack(uint32_t v) { return __half22float2(*reinterpret_cast<const __half2*>(&v)); }
+  // the product alone, and added to c
+  static __device__ __forceinline__ void product(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+                 : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.0f));
+  }
   static __device__ __forceinline__ void mma(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
@@ -439,6 +444,10 @@ template <> struct Half<__nv_bfloat16> {
     return *reinterpret_cast<const uint32_t*>(&v);
   }
   static __device__ __forceinline__ float2 unpack(uint32_t v) { return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xFFFF0000u)); }
+  static __device__ __forceinline__ void product(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+                 : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.0f));
+  }
   static __device__ __forceinline__ void mma(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
@@ -475,13 +484,18 @@ struct HalfShape {
 // lane's scores, maxima and sums belong to the same two heads, so that nothing is exchanged to rescale them.  The weights
 // go from one shape to the other by transposing 8 x 8 matrices, as 16-bit parts that add up to them: three in bf16, all their
 // bits, two in fp16, to 2^-22 (see Half).  Fewer would cost 2^-17 (bf16) of sum w |v|, more than the rounding of the result where
-// values cancel.  Further products are hidden behind the loads with up to eight query heads a key head; with sixteen the third
-// one takes its time (2 GB of bf16 heads of 256 473 us with two, 507 with three; of 128 353 and 375, of 64 355 and 376).
+// values cancel.  A matrix instruction cuts off what it adds up, always to the same side, so that a sum that went through
+// thousands of them would drift (128 requests of up to 24000 tokens: 0.65 % of the results in bf16 one step off, 0.03 % as it
+// is): a tile's products start from zero and are added to the sums before them by rounding additions.  With up to eight
+// query heads a key head the third part and the additions are hidden behind the loads (2 GB of bf16 heads of 256 331 us without
+// both, 360 with; of 128 and 64 no difference); with sixteen they take their time (of 256 471 and 661, of 128 355 and 376, of 64
+// 357 and 376).
 template <class T, int DP, int NT, int WAYS>
 __global__ void __launch_bounds__(kThreads, HalfShape<DP, NT, WAYS>::kResident) k_attention_half(AttentionArgs a) {
   using H = Half<T>;
   using S = HalfShape<DP, NT, WAYS>;
   constexpr int MT = S::kMats;
+  constexpr int KS = 2;                        // steps of sixteen dimensions at a time: products that do not wait for one another
   extern __shared__ __align__(128) unsigned char shared[];
   __shared__ long long scan[kWarps];
   __shared__ Place place;
@@ -664,20 +678,30 @@ __global__ void __launch_bounds__(kThreads, HalfShape<DP, NT, WAYS>::kResident) 
         for (int t = 0; t < MT; ++t) split(w[t], [&](int p, int i) -> uint32_t& { return parts[p][t][n][i]; });
       }
 #pragma unroll
-      for (int k = 0; k < DP / 16; k += 2) {   // two at a time: sums that do not wait for one another (551 us for 507 above)
+      for (int k = 0; k < DP / 16; k += KS) {
+        float c[KS][NT][4];
 #pragma unroll
         for (int t = 0; t < MT; ++t) {
-          uint32_t f[2][4];
+          uint32_t f[KS][4];
 #pragma unroll
-          for (int i = 0; i < 2; ++i)
+          for (int i = 0; i < KS; ++i)
             load_matrices_transposed(f[i], values + (t * 16 + v_row) * S::kRowBytes + ((((k + i) * 2 + v_half) ^ (v_row & 7)) << 4));
 #pragma unroll
           for (int p = 0; p < H::kParts; ++p)
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
+            for (int i = 0; i < KS; ++i)
 #pragma unroll
-              for (int n = 0; n < NT; ++n) H::mma(o[n][k + i], f[i], parts[p][t][n][0], parts[p][t][n][1]);
+              for (int n = 0; n < NT; ++n) {
+                if (t == 0 && p == 0) H::product(c[i][n], f[i], parts[p][t][n][0], parts[p][t][n][1]);
+                else H::mma(c[i][n], f[i], parts[p][t][n][0], parts[p][t][n][1]);
+              }
         }
+#pragma unroll
+        for (int i = 0; i < KS; ++i)
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) o[n][k + i][j] += c[i][n][j];
       }
     }
     __syncwarp();                              // the stage may be filled again

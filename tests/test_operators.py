@@ -1112,3 +1112,35 @@ def test_paged_attention_to_values_that_cancel(B_, dtype):
     bound = scale_of * (2.0 ** -22 + 8 * 2.0 ** -23 + (2.0 ** -22 if dtype == "f16" else 0.0)) + np.abs(exact) * (EPS[dtype] / 2 + 4 * 2.0 ** -23) + TINY[dtype]
     err = np.abs(O.widen(gpu(prog, d)["out"], dtype) - exact) / (bound * (1 + 2.0 ** -7))
     assert np.all(err <= 1), float(err.max())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", REAL)
+def test_paged_attention_adds_up_many_tokens_without_drifting(dtype):
+    """The second half of the tokens has the keys of the first half and values of the other sign: sums that grow to A and come back
+    to nothing, so that what is left are the errors of the additions.  Every tile has the largest score, and scores are exact: no sum
+    is multiplied on the way, and the weights of both halves are the same.
+
+    An addition that rounds to nearest is off by 2^-24 of A at most, either way: of N of them all M results stay within
+    2^-23 A sqrt(N / 2 ln(2 M / d)) with a probability of 1 - d (Hoeffding), d = 10^-9.  Within a tile of 32 tokens six matrix
+    instructions may cut off 17 addends at 2^-24 of the tile's sum each, half of them to the same side as the others; the tiles'
+    sums are 2 A.  Eight more for warps and records."""
+    n, block, B_, hk, D = 20000, 16, 300, 4, 64
+    rng = np.random.default_rng(14)
+    half = n // 2
+    d = _attention_inputs(rng, 1, hk, hk, D, block, [n], dtype)
+    q, keys, values = np.zeros((1, hk, D)), np.zeros((d["keys"].shape[0], hk, D)), np.zeros((d["keys"].shape[0], hk, D))
+    q[:, :, 0] = 1
+    at = d["table"][0, np.arange(n) // block] * block + np.arange(n) % block
+    scores, v = -3 * rng.random((half, hk)), rng.uniform(1, 2, (half, hk, D))
+    scores[::16] = 0
+    keys[at[:half], :, 0] = keys[at[half:], :, 0] = scores
+    values[at[:half]], values[at[half:]] = v, -v
+    d |= {"q": to_type(q.reshape(1, -1), dtype), "keys": to_type(keys.reshape(-1, hk * D), dtype), "values": to_type(values.reshape(-1, hk * D), dtype)}
+    one = _powers_of_two((1, hk, hk, D, block), d, dtype)
+    a = oracle(one, d).abs_sum[5] / 2
+    many = d | {"q": np.repeat(d["q"], B_, 0), "table": np.repeat(d["table"], B_, 0), "lens": np.repeat(d["lens"], B_)}
+    got = O.widen(gpu(_powers_of_two((B_, hk, hk, D, block), many, dtype), many)["out"], dtype)
+    adds = n if dtype == "f32" else n // 32
+    bound = a * (2.0 ** -23 * np.sqrt(adds / 2 * np.log(2 * got.size / 1e-9)) + 2 * 6 * 17 / 2 * 2.0 ** -24 + 8 * 2.0 ** -24) + TINY[dtype]
+    assert np.all(np.abs(got) <= bound * (1 + 2.0 ** -7)), float((np.abs(got) / bound).max())

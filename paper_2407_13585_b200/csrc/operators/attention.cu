@@ -1009,6 +1009,26 @@ __global__ void __launch_bounds__(kThreads, FloatShape<DP, HEADS>::kResident) k_
   if (a.parts && !a.by_unit && threadIdx.x == 0) a.joins[blockIdx.x] = join;
 }
 
+// No query heads, and so no result: only the lengths and the blocks of the tokens attended to are looked at.  A block of the
+// grid to a request.
+__global__ void __launch_bounds__(kThreads) k_attended_blocks(AttentionArgs a) {
+  follow();
+  bool bad = false;
+  for (int b = blockIdx.x; b < a.B; b += gridDim.x) {
+    const int length = a.lens[b];
+    bad = bad || length < 0 || length > (long long)a.W * a.block.d;
+    const Span s = span_of(a, b);
+    if (s.first == s.end) continue;
+    const uint32_t last = (uint32_t)(s.end - 1) / a.block;
+    for (uint32_t p = (uint32_t)s.first / a.block + threadIdx.x; p <= last; p += kThreads) {
+      const int page = a.table[(size_t)b * a.W + p];
+      const uint32_t inside = p < last ? a.block.d - 1 : (uint32_t)(s.end - 1) - last * a.block.d;      // the block's last token
+      bad = bad || page < 0 || (long long)page * a.block.d + inside >= a.S;
+    }
+  }
+  if (bad) raise_index(a.report);
+}
+
 // ---- launches ------------------------------------------------------------------------------------------------------------
 
 AttentionArgs arguments(const ClusterLaunch& L) {
@@ -1106,13 +1126,19 @@ auto choose(const ClusterLaunch& L, F f) {
 
 bool nothing(const ClusterLaunch& L) { return L.op.shape[0] == 0 || L.op.shape[1] == 0; }
 
+int launch_checks(const ClusterLaunch& L) {
+  const AttentionArgs a = arguments(L);
+  if (a.B == 0) return ACC_OK;
+  return launch_following(k_attended_blocks, dim3((unsigned)std::min(a.B, sm_count() * 8)), kThreads, 0, L.stream, a);
+}
+
 int64_t attention_scratch(const ClusterLaunch& L) {
   if (nothing(L)) return 0;
   return choose(L, [&](auto, auto dp, auto shape, auto) { return scratch_of<decltype(shape), decltype(dp)::value>(arguments(L)); });
 }
 
 int launch_attention(const ClusterLaunch& L) {
-  if (nothing(L)) return ACC_OK;
+  if (nothing(L)) return launch_checks(L);
   return choose(L, [&](auto t, auto dp, auto shape, auto kernel) {
     static std::atomic<uint64_t> allowed{0};
     return run<decltype(t), decltype(dp)::value, decltype(shape)>(L, kernel, allowed);

@@ -89,6 +89,9 @@ int allow_shared(K kernel, size_t bytes, std::atomic<uint64_t>& devices) {
   return ACC_OK;
 }
 
+// Reports the numbers x[0 .. n) from `bound` on, for operators whose result has no elements: one launch, if n > 0.
+int report_beyond(const ClusterLaunch& L, const int* x, int64_t n, int bound);
+
 inline int64_t no_scratch(const ClusterLaunch&) { return 0; }
 
 struct Register {

@@ -336,8 +336,11 @@ int launch_marked(const ClusterLaunch& L, PenaltyArgs a) {
 constexpr int64_t kTwoKernels = 1 << 22;
 template <class T>
 int launch(const ClusterLaunch& L) {
-  if (L.op.shape[0] == 0 || L.op.shape[1] == 0) return ACC_OK;
   PenaltyArgs a = arguments(L);
+  if (L.op.shape[0] == 0 || L.op.shape[1] == 0) {
+    const int rc = report_beyond(L, a.tokens, L.op.shape[0] * a.L, a.V);
+    return rc == ACC_OK ? report_beyond(L, a.ids, L.op.shape[0] * a.K, a.V) : rc;
+  }
   const int64_t marks = (int64_t)a.L + a.K;
   if (marks == 0) return launch<T, 256, false>(L, a);
   if (L.op.shape[0] * L.op.shape[1] >= kTwoKernels && 3 * marks <= 2 << kMaxTableBits) {

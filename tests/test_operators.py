@@ -1144,3 +1144,39 @@ def test_paged_attention_adds_up_many_tokens_without_drifting(dtype):
     adds = n if dtype == "f32" else n // 32
     bound = a * (2.0 ** -23 * np.sqrt(adds / 2 * np.log(2 * got.size / 1e-9)) + 2 * 6 * 17 / 2 * 2.0 ** -24 + 8 * 2.0 ** -24) + TINY[dtype]
     assert np.all(np.abs(got) <= bound * (1 + 2.0 ** -7)), float((np.abs(got) / bound).max())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", REAL)
+def test_numbers_outside_their_range_are_reported_where_results_have_no_elements(dtype):
+    def run(prog, d, reported):
+        assert gpu(prog, d, reported=reported)[prog.nodes[prog.outputs[0]].name].size == 0
+    for S, C in ((0, 4), (0, 0), (3, 0)):
+        for slots, reported in ((ints(-1, -5), False), (ints(-1, S), True), (ints(2 ** 31 - 1, -1), True), (ints(0, 0), S == 0)):
+            run(_put_program(S, C, 2, dtype), {"dest": to_type(np.zeros((S, C)), dtype), "slots": slots, "rows": to_type(np.zeros((2, C)), dtype)}, reported)
+        many = np.full(1000, -1, np.int32)
+        for at in (0, 999):
+            run(_put_program(S, C, 1000, dtype), {"dest": to_type(np.zeros((S, C)), dtype), "slots": np.where(np.arange(1000) == at, S, many).astype(np.int32),
+                                                  "rows": to_type(np.zeros((1000, C)), dtype)}, True)
+    d = {"logits": to_type(np.zeros((2, 0)), dtype), "tokens": np.full((2, 700), -1, np.int32), "params": np.ones((2, 4), np.float32),
+         "bias_ids": np.full((2, 3), -1, np.int32), "bias": np.zeros((2, 3), np.float32), "mask": np.zeros((2, 0), np.uint32)}
+    prog = W.penalized_logits(2, 0, 700, 3, True, dtype)
+    run(prog, d, False)
+    for name, at, number in (("tokens", (1, 699), 0), ("tokens", (0, 0), 2 ** 31 - 1), ("bias_ids", (1, 2), 0), ("bias_ids", (0, 1), 9)):
+        bad = {k: v.copy() for k, v in d.items()}
+        bad[name][at] = number
+        run(prog, bad, True)
+    # no query heads: ten slots of a cache in blocks of four, three blocks and a window
+    for hk, window in ((2, 0), (2, 3), (0, 0)):
+        prog = W.paged_attention(3, 0, hk, 16, 10, 4, 3, dtype, 1.0, window)
+        d = {"q": to_type(np.zeros((3, 0)), dtype), "keys": to_type(np.zeros((10, hk * 16)), dtype), "values": to_type(np.zeros((10, hk * 16)), dtype),
+             "table": ints(0, 1, 2, 1, -1, -1, -1, 9, -1).reshape(3, 3), "lens": ints(10, 4, 0)}
+        run(prog, d, False)                                  # (the last block is short of two slots, which nobody attends to)
+        for name, at, number in (("lens", (1,), -1), ("lens", (0,), 13), ("lens", (1,), 2 ** 31 - 1), ("lens", (0,), 11), ("lens", (1,), 5),
+                                 ("table", (0, 2), -1), ("table", (0, 2), 3), ("table", (0, 2), 2 ** 31 - 1)):
+            bad = {k: v.copy() for k, v in d.items()}
+            bad[name][at] = number
+            assert any(O.attended_slots(prog.nodes[5], bad["table"][r].astype(np.int64), bad["lens"][r], 10)[1] for r in range(3))
+            run(prog, bad, True)
+        d["table"][0, 0] = -1                                # in front of the window
+        run(prog, d, window == 0)

@@ -1128,7 +1128,7 @@ bool nothing(const ClusterLaunch& L) { return L.op.shape[0] == 0 || L.op.shape[1
 
 int launch_checks(const ClusterLaunch& L) {
   const AttentionArgs a = arguments(L);
-  if (a.B == 0) return ACC_OK;
+  if (a.B == 0) return no_launch(L);
   return launch_following(k_attended_blocks, dim3((unsigned)std::min(a.B, sm_count() * 8)), kThreads, 0, L.stream, a);
 }
 

@@ -16,6 +16,7 @@ __global__ void __launch_bounds__(256) k_look_over(Report report, const int* x, 
 
 int report_beyond(const ClusterLaunch& L, const int* x, int64_t n, int bound) {
   if (n == 0) return ACC_OK;
+  ++L.extra_launches;
   const int grid = (int)std::min<int64_t>((n + 255) / 256, (int64_t)sm_count() * 8);
   return launch_following(k_look_over, dim3(grid), 256, 0, L.stream, report_of(L), x, n, bound);
 }

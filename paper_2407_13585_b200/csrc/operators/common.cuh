@@ -89,7 +89,14 @@ int allow_shared(K kernel, size_t bytes, std::atomic<uint64_t>& devices) {
   return ACC_OK;
 }
 
-// Reports the numbers x[0 .. n) from `bound` on, for operators whose result has no elements: one launch, if n > 0.
+// An operator's entry counts one launch: for a run without any.
+inline int no_launch(const ClusterLaunch& L) {
+  L.extra_launches = -1;
+  return ACC_OK;
+}
+
+// Reports the numbers x[0 .. n) from `bound` on, for operators whose result has no elements: one launch, if n > 0, counted
+// in extra_launches.
 int report_beyond(const ClusterLaunch& L, const int* x, int64_t n, int bound);
 
 inline int64_t no_scratch(const ClusterLaunch&) { return 0; }

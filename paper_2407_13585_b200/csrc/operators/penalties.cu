@@ -338,6 +338,7 @@ template <class T>
 int launch(const ClusterLaunch& L) {
   PenaltyArgs a = arguments(L);
   if (L.op.shape[0] == 0 || L.op.shape[1] == 0) {
+    no_launch(L);
     const int rc = report_beyond(L, a.tokens, L.op.shape[0] * a.L, a.V);
     return rc == ACC_OK ? report_beyond(L, a.ids, L.op.shape[0] * a.K, a.V) : rc;
   }

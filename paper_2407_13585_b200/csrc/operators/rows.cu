@@ -102,7 +102,7 @@ int64_t put_rows_scratch(const ClusterLaunch& L) { return slot(L, 1).C > kRowsTh
 int launch_put_rows(const ClusterLaunch& L) {
   const size_t e = element_bytes(L.op.dtype);
   const size_t row_bytes = (size_t)L.op.shape[1] * e, bytes = row_bytes * L.op.shape[0];
-  if (bytes == 0) return report_beyond(L, slot_ptr<int>(L, 1), slot(L, 1).C, (int)L.op.shape[0]);
+  if (bytes == 0) return no_launch(L), report_beyond(L, slot_ptr<int>(L, 1), slot(L, 1).C, (int)L.op.shape[0]);
   int launches = 0, rc = ACC_OK;
   const ClusterLaunch* both[2] = {&L, L.also};
   for (int k = 0; k < (L.also ? 2 : 1) && rc == ACC_OK; ++k) {

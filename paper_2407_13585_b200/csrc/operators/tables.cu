@@ -118,7 +118,7 @@ __global__ void __launch_bounds__(kThreads) k_block_table(TableArgs a) {
 int launch_block_table(const ClusterLaunch& L) {
   const dev::NodeArg& t = L.nodes[L.result];
   const long long count = (long long)L.op.shape[0] * L.op.shape[1];
-  if (L.op.shape[0] == 0) return ACC_OK;
+  if (L.op.shape[0] == 0) return no_launch(L);
   const bool grow = L.op.n_inputs == 4;
   TableArgs a{report_of(L), slot_ptr<int>(L, 0), slot_ptr<int>(L, 1), grow ? slot_ptr<int>(L, 2) : nullptr, grow ? slot_ptr<int>(L, 3) : nullptr,
               result_ptr<int>(L), t.R, t.C, (int)slot(L, 1).C, 0, divisor((uint32_t)L.op.iparam[0]), divisor((uint32_t)std::max<int64_t>(L.op.shape[1], 1))};
@@ -284,7 +284,7 @@ int launch_slot_map(const ClusterLaunch& L) {
   const dev::NodeArg& table = slot(L, 0);
   SlotArgs a{report_of(L), slot_ptr<int>(L, 0), slot_ptr<int>(L, 1), slot_ptr<int>(L, 2), result_ptr<int>(L),
              table.R, table.C, (int)L.op.shape[0], divisor((uint32_t)L.op.iparam[0])};
-  if (a.T == 0) return ACC_OK;
+  if (a.T == 0) return no_launch(L);
   const bool single = a.T <= kSingleTokens;
   const int tile = single ? kThreads : 16 * kThreads;
   return launch_following(single ? k_slot_map<1> : k_slot_map<16>, dim3((unsigned)(((long long)a.T + tile - 1) / tile)), kThreads, 0, L.stream, a);

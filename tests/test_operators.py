@@ -1180,3 +1180,22 @@ def test_numbers_outside_their_range_are_reported_where_results_have_no_elements
             run(prog, bad, True)
         d["table"][0, 0] = -1                                # in front of the window
         run(prog, d, window == 0)
+
+
+@pytest.mark.gpu
+def test_launches_of_arrays_of_no_elements_are_not_counted():
+    def launches(prog, into=None):
+        d = {prog.nodes[i].name: np.zeros(prog.nodes[i].shape, {"f32": np.float32, "u32": np.uint32}.get(prog.nodes[i].dtype, np.int32)) for i in prog.input_ids()}
+        b = Bound(prog, d, into)
+        b.g.run(B.FUSED)
+        return b.g.launch_count()
+    assert launches(W.block_tables(0, 4, 3, 5, 4)) == 1      # only the slots of the five tokens of padding
+    assert launches(W.block_tables(0, 4, 3, 0, 4)) == 0
+    assert launches(W.block_tables(3, 4, 3, 0, 4)) == 1
+    assert launches(_put_program(5, 4, 0, "f32"), {"out": "dest"}) == 0
+    assert launches(_put_program(5, 4, 0, "f32")) == 1       # the copy
+    assert launches(_put_program(0, 4, 0, "f32")) == 0
+    assert launches(W.paged_attention(0, 4, 2, 16, 8, 4, 2, "f32")) == 0
+    assert launches(W.penalized_logits(0, 9, 3, 2, True)) == 0
+    assert launches(W.penalized_logits(2, 0, 0, 0, True)) == 0
+    assert launches(W.penalized_logits(2, 9, 0, 0, True)) == 1

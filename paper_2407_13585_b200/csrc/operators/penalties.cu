@@ -17,38 +17,55 @@ struct PenaltyArgs {
   const float* bias;
   const uint32_t* mask;
   void* out;
+  float* sums;         // [B, K]: of the biases of a column, at the number of its first one
   int V, L, K, M;
   int cols, blocks;    // columns of a block, blocks of a row
   int table_bits;      // k_penalize_marked: log2 of the places of a block's table
 };
 
-// A logit that occurs c times (the top bit: also among the first `prompt` tokens) and whose first bias is number `first`.
-__device__ __forceinline__ float changed(const PenaltyArgs& a, int b, int v, float x, uint32_t c, int first, float bias_of_first, bool repeated, const float4& p) {
+// A logit that occurs c times (the top bit: also among the first `prompt` tokens) and the sum of its biases, -0 if it has
+// none: x + -0 is x for every x.
+__device__ __forceinline__ float changed(float x, uint32_t c, float bias, const float4& p) {
   if (c) {
     x = x > 0 ? __fdiv_rn(x, p.x) : __fmul_rn(x, p.x);
     const uint32_t times = c & 0x7FFFFFFFu;
     if (times) x = __fsub_rn(__fsub_rn(x, __fmul_rn(p.y, (float)times)), p.z);
   }
-  if (first != kNoBias) {
-    const int* ids = a.ids + (size_t)b * a.K;
-    const float* bias = a.bias + (size_t)b * a.K;
-    float sum = bias_of_first;
-    if (repeated)
-#pragma unroll 1
-      for (int j = first + 1; j < a.K; ++j)
-        if (ids[j] == v) sum = __fadd_rn(sum, bias[j]);
-    x = __fadd_rn(x, sum);
+  return __fadd_rn(x, bias);
+}
+
+// By a whole warp: bias number k of a row goes to a column, if it is `mine`.  The first bias of a column leaves its number in
+// the column's link, and the column's sum is kept at that number; a lane adds up for all lanes of its column, in their order.
+// So every bias is looked at once, however often a column occurs (searched for in the rest of the list instead, 65535 biases
+// of a row take 38 ms with one column twice; so 0.9).
+__device__ __forceinline__ void add_bias(bool mine, int column, uint16_t* link, int k, float bias, float* sums) {
+  const int lane = threadIdx.x & 31;
+  const uint32_t same = __match_any_sync(~0u, mine ? column : -1 - lane);
+  const bool adds = mine && lane == __ffs(same) - 1;
+  const int had = adds ? *link : kNoBias;
+  uint32_t left = adds ? same : 0;
+  float sum = bias;
+  if (__any_sync(~0u, had != kNoBias || (left & (left - 1)))) {
+    sum = had != kNoBias ? sums[had] : -0.0f;
+    while (__any_sync(~0u, left)) {
+      const float next = __shfl_sync(~0u, bias, left ? __ffs(left) - 1 : 0);
+      if (left) sum = __fadd_rn(sum, next);
+      left &= left - 1;
+    }
   }
-  return x;
+  if (adds) {
+    if (had == kNoBias) *link = (uint16_t)k;
+    sums[had == kNoBias ? k : had] = sum;
+  }
+  __syncwarp();
 }
 
 // A block takes `cols` columns of one row.  They are read, masked and written as they come; meanwhile it goes through the
 // row's tokens: words of shared memory for the columns that occur (and only those) are cleared, then counted up, integer
-// atomics whose order does not matter; who finds a column unmarked puts it on a list.  Of several biases of a column the
-// first one's number is kept; the others, if there are any, are looked for in list order.  At last the columns of the list
-// are read back, changed and written again.  (Done for every element of a vector in turn instead, the code is so long that
-// a block waits for instructions: 256 rows of 131072 bf16 logits and 4096 tokens 151 us.)  Bound: reading and writing the
-// logits; the tokens are read once per block, from L2.
+// atomics whose order does not matter; who finds a column unmarked puts it on a list.  One warp adds up the biases in list
+// order.  At last the columns of the list are read back, changed and written again.  (Done for every element of a vector in
+// turn instead, the code is so long that a block waits for instructions: 256 rows of 131072 bf16 logits and 4096 tokens 151
+// us.)  Bound: reading and writing the logits; the tokens are read once per block, from L2.
 template <class T, int THREADS, bool MARKS>
 __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_penalize(PenaltyArgs a) {
   constexpr int E = 16 / sizeof(T), kCols = THREADS * kVectors * E;
@@ -56,7 +73,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_penalize(PenaltyArg
   uint32_t* touched = count + (a.L > 0 ? kCols : 0);                        // [kCols / 32]
   uint16_t* link = reinterpret_cast<uint16_t*>(touched + kCols / 32);       // [kCols]: the first bias of a column
   uint16_t* list = link + (a.K > 0 ? kCols : 0);                            // the marked columns: no more than L + K, or kCols
-  __shared__ int listed, repeated;
+  __shared__ int listed;
   const int b = blockIdx.x / a.blocks;
   const int v0 = (blockIdx.x - b * a.blocks) * a.cols, v1 = min(v0 + a.cols, a.V);
   // vectors lie on 16 bytes of the whole array, a row may start between two of them: column v is word v - origin
@@ -69,6 +86,8 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_penalize(PenaltyArg
   T* to = static_cast<T*>(a.out) + row;
   const int* tokens = a.tokens + (size_t)b * a.L;
   const int* ids = a.ids + (size_t)b * a.K;
+  const float* biases = a.bias + (size_t)b * a.K;
+  float* sums = a.sums + (size_t)b * a.K;
   const uint32_t* mask = a.mask + (size_t)b * a.M;
   Vector in[kVectors];
   uint32_t bits[kVectors][2];                      // the words that hold a vector's bits
@@ -83,13 +102,15 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_penalize(PenaltyArg
   if constexpr (MARKS)
 #pragma unroll
     for (int k = 0; k < kHeld; ++k) held[k] = k * THREADS + (int)threadIdx.x < a.L ? tokens[k * THREADS + threadIdx.x] : -1;
-  // the warp that goes through the biases has the last of them at hand
-  const int bias_lane = (int)threadIdx.x - (THREADS - 32), last_bias = (a.K - 1) / 32 * 32 + bias_lane;
-  const int last_id = MARKS && a.K > 0 && bias_lane >= 0 && last_bias < a.K ? ids[last_bias] : -1;
+  // the warp that goes through the biases has the first of them at hand
+  const int bias_lane = (int)threadIdx.x - (THREADS - 32);
+  const bool has_bias = MARKS && bias_lane >= 0 && bias_lane < a.K;
+  int id = has_bias ? ids[bias_lane] : -1;
+  float bias = has_bias ? biases[bias_lane] : 0.0f;
   const uint32_t width = v1 - v0;
   if constexpr (MARKS) {
     for (int i = threadIdx.x; i < kCols / 32; i += THREADS) touched[i] = 0;
-    if (threadIdx.x == 0) listed = repeated = 0;
+    if (threadIdx.x == 0) listed = 0;
     bool bad = false;
     const auto clear = [&](int v) {
       if ((uint32_t)(v - v0) < width) {
@@ -145,19 +166,15 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_penalize(PenaltyArg
   for (int k = 0; k < kHeld; ++k) note(held[k], k * THREADS + threadIdx.x);
 #pragma unroll 4
   for (int i = kHeld * THREADS + threadIdx.x; i < a.L; i += THREADS) note(tokens[i], i);
-  if (bias_lane >= 0 && a.K > 0) {                             // from the last bias to the first, 32 at a time
-    const int lane = bias_lane;
-    int v = last_id;
-    for (int k = last_bias; k >= lane; k -= 32) {
-      const int before = k >= 32 + lane ? ids[k - 32] : -1;
-      const bool mine = (uint32_t)(v - v0) < width;
-      const uint32_t same = __match_any_sync(~0u, mine ? v : -1 - lane);
-      if (mine && ((same & (same - 1)) || link[v - origin] != kNoBias)) repeated = 1;
-      __syncwarp();
-      if (mine && lane == __ffs(same) - 1) link[v - origin] = (uint16_t)k;
-      if (mine) put_on_list(v - origin);
-      __syncwarp();
-      v = before;
+  if (bias_lane >= 0) {                                        // 32 at a time
+    for (int k = bias_lane; k < a.K + bias_lane; k += 32) {
+      const bool more = k + 32 < a.K;
+      const int next_id = more ? ids[k + 32] : -1;
+      const float next_bias = more ? biases[k + 32] : 0.0f;
+      const bool mine = (uint32_t)(id - v0) < width;
+      if (mine) put_on_list(id - origin);
+      if (__any_sync(~0u, mine)) add_bias(mine, id, link + (mine ? id - origin : 0), k, bias, sums);
+      id = next_id, bias = next_bias;
     }
   }
   __syncthreads();
@@ -167,7 +184,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_penalize(PenaltyArg
     const int w = list[i], v = origin + w;
     if (a.M > 0 && !(mask[v >> 5] >> (v & 31) & 1)) continue;
     const int bias = a.K > 0 ? link[w] : kNoBias;
-    to[v] = narrow<T>(changed(a, b, v, widen<T>(to[v]), a.L > 0 ? count[w] : 0, bias, bias != kNoBias ? a.bias[(size_t)b * a.K + bias] : 0.0f, repeated, p));
+    to[v] = narrow<T>(changed(widen<T>(to[v]), a.L > 0 ? count[w] : 0, bias != kNoBias ? sums[bias] : -0.0f, p));
   }
 }
 
@@ -178,6 +195,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_penalize(PenaltyArg
 // table.  Which place a column gets depends on the order of the threads, what is written to it does not.
 constexpr int kMarkedThreads = 512, kMaxTableBits = 14, kMaxTableBytes = (10 << kMaxTableBits) + (4 << kMaxTableBits) / 3;
 constexpr int kEmptyPlace = -1;
+constexpr size_t kThirdOfAnSM = 77 << 10;   // shared memory that three blocks of an SM cannot have
 template <class T>
 __global__ void __launch_bounds__(kMarkedThreads, 2) k_penalize_marked(PenaltyArgs a) {
   extern __shared__ __align__(16) uint32_t count[];                         // [places]
@@ -185,18 +203,22 @@ __global__ void __launch_bounds__(kMarkedThreads, 2) k_penalize_marked(PenaltyAr
   int* key = reinterpret_cast<int*>(count + places);                        // [places]: the column
   uint16_t* link = reinterpret_cast<uint16_t*>(key + places);               // [places]: the first bias of a column
   uint16_t* list = link + (a.K > 0 ? places : 0);                           // the places that were taken: no more than L + K
-  __shared__ int listed, repeated;
+  __shared__ int listed;
   const int b = blockIdx.x / a.blocks;
   const int v0 = (blockIdx.x - b * a.blocks) * a.cols, v1 = min(v0 + a.cols, a.V);
   const uint32_t width = v1 - v0;
   const int* tokens = a.tokens + (size_t)b * a.L;
   const int* ids = a.ids + (size_t)b * a.K;
+  const float* biases = a.bias + (size_t)b * a.K;
+  float* sums = a.sums + (size_t)b * a.K;
   const uint32_t* mask = a.mask + (size_t)b * a.M;
   int held[kHeld];
 #pragma unroll
   for (int k = 0; k < kHeld; ++k) held[k] = k * kMarkedThreads + (int)threadIdx.x < a.L ? tokens[k * kMarkedThreads + threadIdx.x] : -1;
-  const int bias_lane = (int)threadIdx.x - (kMarkedThreads - 32), last_bias = (a.K - 1) / 32 * 32 + bias_lane;
-  int id = a.K > 0 && bias_lane >= 0 && last_bias < a.K ? ids[last_bias] : -1;
+  const int bias_lane = (int)threadIdx.x - (kMarkedThreads - 32);
+  const bool has_bias = bias_lane >= 0 && bias_lane < a.K;
+  int id = has_bias ? ids[bias_lane] : -1;
+  float bias = has_bias ? biases[bias_lane] : 0.0f;
   const float4 p = *reinterpret_cast<const float4*>(a.params + 4 * (size_t)b);
   // (64 places at least: every array is a multiple of 16 bytes)
   for (int i = threadIdx.x; i < places / 4; i += kMarkedThreads) {
@@ -205,7 +227,7 @@ __global__ void __launch_bounds__(kMarkedThreads, 2) k_penalize_marked(PenaltyAr
   }
   if (a.K > 0)
     for (int i = threadIdx.x; i < places / 8; i += kMarkedThreads) reinterpret_cast<uint4*>(link)[i] = make_uint4(~0u, ~0u, ~0u, ~0u);
-  if (threadIdx.x == 0) listed = repeated = 0;
+  if (threadIdx.x == 0) listed = 0;
   __syncthreads();
   const int prompt = (int)fminf(fmaxf(p.w, 0.0f), 2147483520.0f);
   bool bad = false;
@@ -247,22 +269,18 @@ __global__ void __launch_bounds__(kMarkedThreads, 2) k_penalize_marked(PenaltyAr
     const int i = i0 + threadIdx.x;
     note(i < a.L ? tokens[i] : -1, i);
   }
-  if (bias_lane >= 0 && a.K > 0) {                 // from the last bias to the first, 32 at a time
-    const int lane = bias_lane;
-    for (int k = last_bias; k >= lane; k -= 32) {
-      const int before = k >= 32 + lane ? ids[k - 32] : -1;
+  if (bias_lane >= 0) {                            // 32 at a time
+    for (int k = bias_lane; k < a.K + bias_lane; k += 32) {
+      const bool more = k + 32 < a.K;
+      const int next_id = more ? ids[k + 32] : -1;
+      const float next_bias = more ? biases[k + 32] : 0.0f;
       bad = bad || id >= a.V;
       const bool mine = (uint32_t)(id - v0) < width;
-      const uint32_t same = __match_any_sync(~0u, mine ? id : -1 - lane);
       bool taken = false;
       const uint32_t place = mine ? place_of(id, taken) : 0;
       put_on_list(taken, place);
-      __syncwarp();
-      if (mine && ((same & (same - 1)) || link[place] != kNoBias)) repeated = 1;
-      __syncwarp();
-      if (mine && lane == __ffs(same) - 1) link[place] = (uint16_t)k;
-      __syncwarp();
-      id = before;
+      if (__any_sync(~0u, mine)) add_bias(mine, id, link + place, k, bias, sums);
+      id = next_id, bias = next_bias;
     }
   }
   if (bad) raise_index(a.report);
@@ -285,20 +303,20 @@ __global__ void __launch_bounds__(kMarkedThreads, 2) k_penalize_marked(PenaltyAr
       word[k] = v[k] < 0 ? 0 : a.M > 0 ? mask[v[k] >> 5] : ~0u;
       c[k] = count[place];
       first[k] = a.K > 0 ? link[place] : kNoBias;
-      bias[k] = first[k] != kNoBias ? a.bias[(size_t)b * a.K + first[k]] : 0.0f;
+      bias[k] = first[k] != kNoBias ? sums[first[k]] : -0.0f;
     }
 #pragma unroll 1
     for (int k = 0; k < kAhead; ++k) {
-      if (word[0] >> (v[0] & 31) & 1) to[v[0]] = narrow<T>(changed(a, b, v[0], x[0], c[0], first[0], bias[0], repeated, p));
+      if (word[0] >> (v[0] & 31) & 1) to[v[0]] = narrow<T>(changed(x[0], c[0], bias[0], p));
 #pragma unroll
-      for (int u = 0; u + 1 < kAhead; ++u) v[u] = v[u + 1], x[u] = x[u + 1], c[u] = c[u + 1], word[u] = word[u + 1], first[u] = first[u + 1], bias[u] = bias[u + 1];
+      for (int u = 0; u + 1 < kAhead; ++u) v[u] = v[u + 1], x[u] = x[u + 1], c[u] = c[u + 1], word[u] = word[u + 1], bias[u] = bias[u + 1];
     }
   }
 }
 
 PenaltyArgs arguments(const ClusterLaunch& L) {
   return {report_of(L), slot(L, 0).ptr, slot_ptr<int>(L, 1), slot_ptr<float>(L, 2), slot_ptr<int>(L, 3), slot_ptr<float>(L, 4),
-          slot_ptr<uint32_t>(L, 5), result_ptr<void>(L), (int)L.op.shape[1], slot(L, 1).C, slot(L, 3).C, slot(L, 5).C, 0, 0, 0};
+          slot_ptr<uint32_t>(L, 5), result_ptr<void>(L), reinterpret_cast<float*>(L.scratch), (int)L.op.shape[1], slot(L, 1).C, slot(L, 3).C, slot(L, 5).C, 0, 0, 0};
 }
 
 template <class T, int THREADS, bool MARKS>
@@ -328,7 +346,10 @@ int launch_marked(const ClusterLaunch& L, PenaltyArgs a) {
   const int rc = allow_shared(k_penalize_marked<T>, (size_t)kMaxTableBytes, allowed);
   if (rc != ACC_OK) return rc;
   ++L.extra_launches;
-  return launch_following(k_penalize_marked<T>, dim3((unsigned)B * (unsigned)a.blocks), kMarkedThreads, bytes(a.table_bits), L.stream, a);
+  // (blocks that two to an SM hold are not put three to those SMs that the copy leaves first: 256 rows, 4096 tokens 70 us, so 43)
+  const unsigned grid = (unsigned)B * (unsigned)a.blocks;
+  const size_t shared = std::max(bytes(a.table_bits), grid <= 2u * sm_count() ? kThirdOfAnSM : 0);
+  return launch_following(k_penalize_marked<T>, dim3(grid), kMarkedThreads, shared, L.stream, a);
 }
 
 // From this many logits on, two kernels (rows of 131072 with a mask; one kernel, two): 256 of bf16 with 4096 tokens 57, 48 us,
@@ -358,7 +379,9 @@ int launch_penalize(const ClusterLaunch& L) {
   return L.op.dtype == ACC_F32 ? launch<float>(L) : L.op.dtype == ACC_F16 ? launch<__half>(L) : launch<__nv_bfloat16>(L);
 }
 
-const Register penalize(ACC_PENALIZE, "k_penalize", no_scratch, launch_penalize);
+int64_t penalties_scratch(const ClusterLaunch& L) { return L.op.shape[1] > 0 ? 4 * L.op.shape[0] * slot(L, 3).C : 0; }
+
+const Register penalize(ACC_PENALIZE, "k_penalize", penalties_scratch, launch_penalize);
 
 }  // namespace
 }  // namespace ops

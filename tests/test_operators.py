@@ -1199,3 +1199,39 @@ def test_launches_of_arrays_of_no_elements_are_not_counted():
     assert launches(W.penalized_logits(0, 9, 3, 2, True)) == 0
     assert launches(W.penalized_logits(2, 0, 0, 0, True)) == 0
     assert launches(W.penalized_logits(2, 9, 0, 0, True)) == 1
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", REAL)
+@pytest.mark.parametrize("B_,V,Lh,K", [(1, 70000, 40, 65535), (2, 9001, 0, 9000), (50, 100000, 30, 5000), (48, 100000, 0, 10921)])
+def test_long_lists_of_biases_with_columns_that_occur_twice(B_, V, Lh, K, dtype):
+    """In list order, far apart and side by side, with one column twice and with every column twice or more; and at a cost that
+    does not depend on how often a column occurs."""
+    import torch
+    rng = np.random.default_rng(K)
+    d = _penalty_inputs(rng, B_, V, Lh, K, True, dtype)
+    d["mask"][:] = 0xFFFFFFFF
+    once = np.stack([rng.permutation(V)[:K] for _ in range(B_)]).astype(np.int32)
+    one, all_of_them = once.copy(), once.copy()
+    one[:, -1] = one[:, 0]
+    all_of_them[:, K // 2:K // 2 * 2] = all_of_them[:, :K // 2]
+    all_of_them[:, 64:96] = all_of_them[:, 64:65]
+    prog = W.penalized_logits(B_, V, Lh, K, True, dtype)
+    b = Bound(prog, d | {"bias_ids": once})
+    times = []
+    for ids in (once, one, all_of_them):
+        b.t["bias_ids"].copy_(to_cuda(ids, "i32"))
+        b.g.run(B.FUSED)
+        if B_ <= 2:
+            _check_penalties(prog, d | {"bias_ids": ids}, b.outputs()["penalized"], dtype)
+        runs = []
+        for _ in range(5):
+            start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            start.record()
+            b.g.run(B.FUSED, finish=False)
+            end.record()
+            end.synchronize()
+            runs.append(start.elapsed_time(end))
+        times.append(sorted(runs)[2])
+    b.g.finish()
+    assert max(times[1:]) <= 3 * times[0] + 0.05, times

@@ -10,6 +10,7 @@
 #include <mutex>
 
 #include "cluster.h"
+#include "division.h"
 #include "exec.h"
 #include "graph.h"
 #include "registry.h"
@@ -64,16 +65,12 @@ static dev::NodeArg node_arg(const Node& n, const void* ptr) {
   a.ip1 = (int32_t)(uint32_t)(n.d.iparam[1] & 0xFFFFFFFFll);
   a.fp0 = (float)n.d.fparam[0];
   a.fp1 = (float)n.d.fparam[1];
-  // branch-free division by d (Granlund and Montgomery's round-up multiplier, 33 bits with the
-  // add-and-shift fix-up): l = ceil(log2 d), m = floor(2^32 (2^l - d) / d) + 1,
-  // v / d = (t + ((v - t) >> min(l, 1))) >> max(l - 1, 0) with t = umulhi(v, m); d = 1 gives v
   const uint32_t d = (uint32_t)(n.d.fn_id == ACC_FN_MUL_MOD ? a.ip1 : a.ip0);
   if (d >= 1) {
-    uint32_t l = 0;
-    while (l < 32 && (1ull << l) < d) ++l;
-    a.div_mul = (uint32_t)((((1ull << l) - d) << 32) / d + 1);
-    a.div_sh1 = l < 1 ? l : 1;
-    a.div_sh2 = l - a.div_sh1;
+    const Divisor by = divisor(d);
+    a.div_mul = by.mul;
+    a.div_sh1 = by.sh1;
+    a.div_sh2 = by.sh2;
     a.div_mask = (d & (d - 1)) == 0 ? d - 1 : 0;
   }
   a.R = n.d.rank == 2 ? (int32_t)n.d.shape[0] : 1;
@@ -235,10 +232,7 @@ int build_schedule(Graph& g, int executor, Schedule& sch) {
       const CNode& op = st.cc.nodes[st.cc.n - 1];
       st.launch.op = g.nodes[st.first_node].d;
       st.launch.result = st.cc.n - 1;
-      for (int s = 0; s < op.nin; ++s) {
-        st.launch.slot[s] = op.in[s];
-        st.launch.slot_dtype[s] = st.cc.nodes[op.in[s]].dtype;
-      }
+      for (int s = 0; s < op.nin; ++s) st.launch.slot[s] = op.in[s];
       const int rc = check_operator_buffers(g, pi, st.first_node);
       if (rc != ACC_OK) return rc;
     }

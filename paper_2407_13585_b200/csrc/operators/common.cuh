@@ -10,6 +10,7 @@
 
 #include "acc.h"
 #include "device/eval.cuh"
+#include "division.h"
 #include "graph.h"
 #include "registry.h"
 
@@ -30,16 +31,6 @@ const T* slot_ptr(const ClusterLaunch& L, int s) { return static_cast<const T*>(
 template <class T>
 T* result_ptr(const ClusterLaunch& L) { return static_cast<T*>(const_cast<void*>(L.nodes[L.result].ptr)); }
 
-// Unsigned division by a constant of the launch: dev::div_by with the multiplier of dev::NodeArg.
-struct Divisor {
-  uint32_t d, mul, sh1, sh2;
-};
-inline Divisor divisor(uint32_t d) {
-  uint32_t l = 0;
-  while (l < 32 && (1ull << l) < d) ++l;
-  const uint32_t sh1 = l < 1 ? l : 1;
-  return {d, (uint32_t)((((1ull << l) - d) << 32) / d + 1), sh1, l - sh1};
-}
 __device__ __forceinline__ uint32_t operator/(uint32_t v, const Divisor& p) {
   const uint32_t t = __umulhi(v, p.mul);
   return (t + ((v - t) >> p.sh1)) >> p.sh2;
@@ -48,9 +39,12 @@ __device__ __forceinline__ uint32_t operator/(uint32_t v, const Divisor& p) {
 // The blocks that `length` tokens take up.
 __device__ __forceinline__ int blocks_of(int length, const Divisor& block) { return length <= 0 ? 0 : (int)((uint32_t)(length - 1) / block) + 1; }
 
-// Launches a kernel so that it may be set up while the one before it in the stream still runs.  It begins with
-// follow(): nothing is read or written before everything that was launched earlier has finished and its results are
-// visible.  (A kernel that begins so may follow another one: each of them ends only after it has waited.)
+// Launches a kernel so that it may be set up while the one before it in the stream still runs.  Most begin with follow():
+// nothing is read or written before everything that was launched earlier has finished and its results are visible.  (A
+// kernel that begins so may follow another one: each of them ends only after it has waited.)  Two read inputs before they
+// wait, each behind a kernel of its own operator that cannot have begun before all inputs were complete: k_put_rows behind
+// k_settle_owners, which is launched plainly, and k_penalize_marked (which also writes its scratch) behind k_penalize, which
+// has waited before it lets the next one start.
 template <class... P, class... A>
 int launch_following(void (*kernel)(P...), dim3 grid, int threads, size_t shared, cudaStream_t stream, const A&... args) {
   cudaLaunchConfig_t config{};

@@ -20,10 +20,9 @@ struct ClusterLaunch {
   uint32_t run_id = 0;
   uint32_t spin_limit = 1u << 22;
   cudaStream_t stream = nullptr;
-  // An operator (graph.h, is_operator): its description, the local ids of its slots and of its result, their types
+  // An operator (graph.h, is_operator): its description, the local ids of its slots and of its result
   acc_node_desc op{};
   int slot[kMaxSlots] = {}, result = 0;
-  int slot_dtype[kMaxSlots] = {};
   const ClusterLaunch* also = nullptr;   // a second operator of this kind and these shapes that the launch takes along (exec.h, together_with_next)
   mutable int extra_launches = 0;   // set by a launcher that took more launches than its entry's `passes` (data-dependent paths)
 };

@@ -242,7 +242,9 @@ int acc_edges(const acc_graph* g, int32_t* F, int32_t* nF, int32_t* I, int32_t* 
  *     D = iparam[1] is a multiple of 8 up to 256, Hq a multiple of Hk.
  *     scale = fparam[0].  iparam[2] > 0: only the last iparam[2] tokens (a sliding
  *     window).  A request without tokens yields zeros.  One element type of F32,
- *     F16, BF16; products, softmax and sums are held in 32 bits.  What a request
+ *     F16, BF16; products, softmax and sums are held in 32 bits: exponentials to 2^-22
+ *     of themselves, and so are, in F16, weights from 2^-36 of the largest on where
+ *     they meet the values (below to 2^-58 of the largest).  What a request
  *     does not attend to may hold anything.  An infinite value that it does attend
  *     to makes its element of the result infinite or not a number.  Reported: a
  *     negative length (no tokens), a length beyond W * block (cut off), a block

@@ -3,9 +3,10 @@
 //   out[b, h] = sum_t w_t v_t / sum_t w_t,   w_t = 2^(s_t - m),   s_t = log2(e) scale q[b, h].k_t,   m = max_t s_t
 //
 // in one pass over keys and values: with a running maximum m, sums and products so far are multiplied by 2^(m - m') when a
-// larger m' turns up, and two runs over different tokens join the same way.  Keys and values are read once (that is what
-// bounds it: 2 e D bytes per token and key head for 4 D (Hq / Hk) operations), so the query heads of a key head are
-// worked on together, eight or sixteen at a time.
+// larger m' turns up, and two runs over different tokens join the same way.  Reading keys and values is what bounds it (2 e D
+// bytes per token and key head for 4 D (Hq / Hk) operations), so the query heads of a key head are worked on together: up to
+// eight or sixteen in 16-bit types, two, four or eight in fp32.  Where a key head has more, they are several units, and each of
+// them goes through the tokens again.
 //
 // Splitting.  The work is the list of all tiles (four warps x 16 or 8 tokens) of all requests and key heads, one unit
 // (request, block of heads) after the other; every block of a grid that fills the GPU once takes an equal run of that
@@ -14,7 +15,8 @@
 // the blocks: no atomics, the same bits every time.
 //
 // Inside a block every warp takes its 16 (8) tokens of a tile through a ring of stages of its own in shared memory, filled
-// by 16-byte asynchronous copies two tiles ahead, across units; the block numbers are read one tile further ahead.
+// by 16-byte asynchronous copies across units, two tiles ahead, or one where there is room for two stages only (16-bit heads of
+// 65 to 96 elements, fp32 heads of 65 to 128); the block numbers are read one tile further ahead.
 #include <cfloat>
 
 #include "operators/common.cuh"

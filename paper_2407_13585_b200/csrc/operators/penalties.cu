@@ -352,8 +352,10 @@ int launch_marked(const ClusterLaunch& L, PenaltyArgs a) {
   return launch_following(k_penalize_marked<T>, dim3(grid), kMarkedThreads, shared, L.stream, a);
 }
 
-// From this many logits on, two kernels (rows of 131072 with a mask; one kernel, two): 256 of bf16 with 4096 tokens 57, 48 us,
-// with 256 tokens 43, 28; 20 of fp32 with 6000 tokens 29, 30; 8 of bf16 with 6000 23, 26.
+// From this many logits on, two kernels (with a mask; one kernel, two, in us).  Rows of 131072: 256 of bf16 with 4096 tokens 54, 48,
+// with 256 tokens 43, 28; 32 of fp32 with 4096 20, 15, of bf16 with 2000 11, 10; 16 of bf16 9.2, 9.5.  Shorter rows, with 20
+// to 64 biases: 256 of 32000 and 2000 tokens 17.4, 18.6; 256 of 16384 and 2000 13.8, 15.7; 1000 of 8000 and 500 18, 20; 2000
+// of 4000 and 500 30, 30; 4000 of 1000 and 300 50, 45, and 4000 76, 95.
 constexpr int64_t kTwoKernels = 1 << 22;
 template <class T>
 int launch(const ClusterLaunch& L) {

@@ -119,7 +119,8 @@ int launch_put_rows(const ClusterLaunch& L) {
   if (a.T > 0 && rc == ACC_OK) {
     if (a.T > kRowsThatLook) {
       a.owner = reinterpret_cast<int*>(L.scratch);
-      // (launched like any other kernel: it begins when everything before it has finished)
+      // launched plainly, and it has to be: it begins when everything before it has finished, so that k_put_rows, which may start
+      // as soon as this one has, finds slots and rows complete without waiting
       k_settle_owners<<<(a.T + 255) / 256, 256, 0, L.stream>>>(a.slots, a.owner, a.T, a.S);
       rc = launched();
       ++launches;

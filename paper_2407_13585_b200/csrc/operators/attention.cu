@@ -419,7 +419,7 @@ template <> struct Half<__half> {
   // more to 2^-22.  Those below (kSmall) are raised by another 2^18 and have products of their own, in tiles that have any:
   // down to 2^-36 they are held to 2^-22 as well, and what is lost of smaller ones is 2^-58 of the maximum at most.  (Raised
   // by 2^12 and without products of their own, weights of 2^-30 were off by 2^-8 and those of 2^-38 were nothing.  Where every
-  // tile has small ones, 31 windows of 20 heads of 80 take 110 us in place of 98, 2 GB under sixteen heads of 256 875, so 620.)
+  // tile has small ones, 31 windows of 20 heads of 80 take 110 us in place of 97, 2 GB under sixteen heads of 256 673 in place of 515.)
   static constexpr int kParts = 2;
   static constexpr float kRaise = 32768.0f, kSmall = 0x1p-3f, kRaiseSmall = 0x1p18f, kNothing = 0x1p-43f;
   static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
@@ -477,7 +477,10 @@ struct HalfShape {
   // stages and resident blocks per SM: as many as 227 KB hold
   static constexpr int kStages = DP == 96 ? 2 : 3;
   static constexpr int kResident = DP == 256 ? 1 : DP == 96 ? 3 : 2;
-  static constexpr int kShared = kWarps * kStages * kStageBytes;
+  // sixteen heads of 256: a lane's queries lie in shared memory, 16 bytes for every sixteen dimensions, because sums and queries
+  // together do not fit its registers beside products that do not wait for one another (2 GB of bf16 660 us, so 501)
+  static constexpr bool kAside = DP == 256 && NT == 2;
+  static constexpr int kRingBytes = kWarps * kStages * kStageBytes, kShared = kRingBytes + (kAside ? kThreads * DP : 0);
   static_assert(WAYS > 1 || kRows * DP * 4 <= kStageBytes, "a warp's sums go through a stage");
 };
 
@@ -490,14 +493,14 @@ struct HalfShape {
 // thousands of them would drift (128 requests of up to 24000 tokens: 0.65 % of the results in bf16 one step off, 0.03 % as it
 // is): a tile's products start from zero and are added to the sums before them by rounding additions.  With up to eight
 // query heads a key head the third part and the additions are hidden behind the loads (2 GB of bf16 heads of 256 331 us without
-// both, 360 with; of 128 and 64 no difference); with sixteen they take their time (of 256 471 and 661, of 128 355 and 376, of 64
+// both, 360 with; of 128 and 64 no difference); with sixteen they take their time (of 256 470 and 501, of 128 355 and 376, of 64
 // 357 and 376).
 template <class T, int DP, int NT, int WAYS>
 __global__ void __launch_bounds__(kThreads, HalfShape<DP, NT, WAYS>::kResident) k_attention_half(AttentionArgs a) {
   using H = Half<T>;
   using S = HalfShape<DP, NT, WAYS>;
   constexpr int MT = S::kMats;
-  constexpr int KS = 2;                        // steps of sixteen dimensions at a time: products that do not wait for one another
+  constexpr int KS = S::kAside ? 4 : 2;                        // steps of sixteen dimensions at a time: products that do not wait for one another
   extern __shared__ __align__(128) unsigned char shared[];
   __shared__ long long scan[kWarps];
   __shared__ Place place;
@@ -532,7 +535,8 @@ __global__ void __launch_bounds__(kThreads, HalfShape<DP, NT, WAYS>::kResident) 
     }
     commit_copies();
   }
-  uint32_t q[NT][DP / 16][2];
+  uint32_t q[NT][S::kAside ? 1 : DP / 16][2];
+  uint4* aside = reinterpret_cast<uint4*>(shared + S::kRingBytes) + threadIdx.x;      // kAside: [DP / 16][kThreads]
   float o[NT][DP / 16][4], m[NT][2], l[NT][2];
   bool fresh = true, from_start = c.tile == 0;
   int stage = 0;
@@ -546,8 +550,9 @@ __global__ void __launch_bounds__(kThreads, HalfShape<DP, NT, WAYS>::kResident) 
         const uint32_t* from = reinterpret_cast<const uint32_t*>(static_cast<const T*>(a.q) + ((size_t)c.b * a.Hq + (size_t)kv * a.group + head) * a.D) + (lane & 3);
 #pragma unroll
         for (int k = 0; k < DP / 16; ++k) {
-          q[n][k][0] = head < a.group && k * 16 < a.D ? from[k * 8] : 0;
-          q[n][k][1] = head < a.group && k * 16 + 8 < a.D ? from[k * 8 + 4] : 0;
+          const uint32_t x = head < a.group && k * 16 < a.D ? from[k * 8] : 0, y = head < a.group && k * 16 + 8 < a.D ? from[k * 8 + 4] : 0;
+          if constexpr (S::kAside) reinterpret_cast<uint2*>(aside + k * kThreads)[n] = make_uint2(x, y);
+          else q[n][k][0] = x, q[n][k][1] = y;
 #pragma unroll
           for (int i = 0; i < 4; ++i) o[n][k][i] = 0;
         }
@@ -585,12 +590,17 @@ __global__ void __launch_bounds__(kThreads, HalfShape<DP, NT, WAYS>::kResident) 
           for (int i = 0; i < 4; ++i) s[t][n][i] = odd[t][n][i] = 0;
 #pragma unroll
       for (int k = 0; k < DP / 16; ++k) {
+        const int at = S::kAside ? 0 : k;
+        if constexpr (S::kAside) {
+          const uint4 x = aside[k * kThreads];
+          q[0][0][0] = x.x, q[0][0][1] = x.y, q[NT - 1][0][0] = x.z, q[NT - 1][0][1] = x.w;
+        }
 #pragma unroll
         for (int t = 0; t < MT; ++t) {
           uint32_t f[4];
           load_matrices(f, keys + (t * 16 + k_row) * S::kRowBytes + (((k * 2 + k_half) ^ (k_row & 7)) << 4));
 #pragma unroll
-          for (int n = 0; n < NT; ++n) H::mma(k & 1 ? odd[t][n] : s[t][n], f, q[n][k][0], q[n][k][1]);
+          for (int n = 0; n < NT; ++n) H::mma(k & 1 ? odd[t][n] : s[t][n], f, q[n][at][0], q[n][at][1]);
         }
       }
       uint32_t parts[H::kParts][MT][NT][2];

@@ -500,7 +500,7 @@ __global__ void __launch_bounds__(kThreads, HalfShape<DP, NT, WAYS>::kResident) 
   using H = Half<T>;
   using S = HalfShape<DP, NT, WAYS>;
   constexpr int MT = S::kMats;
-  constexpr int KS = S::kAside ? 4 : 2;                        // steps of sixteen dimensions at a time: products that do not wait for one another
+  constexpr int KS = S::kAside ? 4 : 2;        // steps of sixteen dimensions at a time: products that do not wait for one another
   extern __shared__ __align__(128) unsigned char shared[];
   __shared__ long long scan[kWarps];
   __shared__ Place place;

@@ -246,7 +246,8 @@ int acc_edges(const acc_graph* g, int32_t* F, int32_t* nF, int32_t* I, int32_t* 
  *     of themselves, and so are, in F16, weights from 2^-36 of the largest on where
  *     they meet the values (below to 2^-58 of the largest).  What a request
  *     does not attend to may hold anything.  An infinite value that it does attend
- *     to makes its element of the result infinite or not a number.  Reported: a
+ *     to makes its element of the result infinite or not a number, and so may values
+ *     whose sum, each weighted relative to the largest weight, passes 2^128.  Reported: a
  *     negative length (no tokens), a length beyond W * block (cut off), a block
  *     outside the cache (its tokens are left out).
  * PENALIZE {logits[B, V], tokens[B, L], params[B, 4], bias_ids[B, K], bias[B, K], mask[B, M]} -> [B, V]
